@@ -337,6 +337,73 @@ size_t et_projector_workspace_bytes(const et_projector *proj, int32_t rows);
 int et_project_tokens(et_projector *proj, const uint16_t *tokens_dev, int32_t rows, void *workspace_dev,
                       size_t workspace_bytes, uint16_t *out_dev, void *hip_stream);
 
+/* ---- the key-value cache of the language model behind the projector ------------------------------
+ * The kept tokens end up as keys and values in a cache that every later token of the answer reads.  The cache is paged:
+ * `n_pages` pages of `page_size` tokens in one device buffer that the caller owns, and a page table that
+ * gives each sequence its pages.  These calls store new keys and values (in 8 bits if asked to), read them
+ * back, and compute the attention of one new token for each sequence.
+ *
+ * A page is et_kv_page_bytes() bytes, one key-value head after the other; a head's part holds
+ *     keys [page_size, head_dim] | values [page_size, head_dim] | key maxima [page_size] | value maxima [page_size],
+ * so pages can be copied, shared and moved as they are.  ET_KV_BF16: keys and values in bfloat16, no maxima.  ET_KV_INT8 and
+ * ET_KV_E4M3: one byte per value (two's complement; OCP 8-bit float with 4 exponent bits); a row x of
+ * head_dim values is held as its largest magnitude m (bfloat16, exact) and the codes round(x * Q / m), ties to even, Q = 127
+ * or 448; it stands for code * m / Q.  A row with an infinity or a NaN has m = NaN and reads back as NaN throughout.
+ *
+ * Token `pos` of sequence b is token pos % page_size of page page_table[b * table_stride + pos / page_size].  An
+ * entry outside [0, n_pages) is no page: nothing is stored there, it reads back as zeros, and attention leaves its tokens out;
+ * so do the calls with positions past pages_per_seq * page_size.  All of this is checked on the device; lengths and
+ * tables stay there, so the calls can be captured into a graph and replayed as the sequences grow.
+ * Sequences may share pages that they only read.  Two rows of one et_kv_append that come to lie in the same place leave
+ * either's values there, and not necessarily those of one row alone.
+ *
+ * Rows: et_kv_append and et_kv_read take the new (or wanted) tokens of all sequences as consecutive rows; rows
+ * cu_rows[b] .. cu_rows[b + 1] are the LAST tokens of sequence b, i.e. row cu_rows[b + 1] - 1 is position kv_len[b] - 1
+ * (kv_len counts the new tokens).  cu_rows_dev = NULL: one row for each sequence (rows = n_seqs).  Rows outside
+ * cu_rows[0] .. cu_rows[n_seqs], such as padding behind the last sequence, are neither read nor written; a row whose
+ * position would be negative (an idle slot of kv_len 0) is not stored and reads back as zeros. */
+enum { ET_KV_BF16 = 0, ET_KV_E4M3 = 1, ET_KV_INT8 = 2 };
+typedef struct {
+  void *data_dev;              /* n_pages * et_kv_page_bytes bytes, aligned to 16                    */
+  int32_t n_pages, page_size;  /* page_size 16, 32, 64, 128 or 256                                   */
+  int32_t n_kv_heads, head_dim; /* head_dim 64, 80, 96, 128 or 256                                   */
+  int32_t format;
+} et_kv_cache;
+typedef struct {
+  const int32_t *page_table_dev; /* [n_seqs, table_stride], of which pages_per_seq columns are used  */
+  int32_t table_stride, pages_per_seq;
+  const int32_t *kv_len_dev; /* [n_seqs]                                                             */
+  int32_t n_seqs;
+} et_kv_seqs;
+
+/* Bytes of one page; 0 on bad arguments. */
+size_t et_kv_page_bytes(int32_t page_size, int32_t n_kv_heads, int32_t head_dim, int32_t format);
+
+/* Store rows of k_dev and v_dev, bf16 [rows, n_kv_heads * head_dim] with row strides in elements (multiples of 8, pointers
+ * aligned to 16 bytes; columns of a fused projection can be passed as they lie).  Asynchronous on `hip_stream`.  Errors:
+ * INVALID_ARG, UNSUPPORTED (page_size, head_dim), HIP. */
+int et_kv_append(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *cu_rows_dev, int32_t rows,
+                 const uint16_t *k_dev, int64_t k_stride, const uint16_t *v_dev, int64_t v_stride, void *hip_stream);
+
+/* The inverse: the values that the cache's rows stand for, rounded to bf16 once.  Same rows, same strides, same errors. */
+int et_kv_read(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *cu_rows_dev, int32_t rows,
+               uint16_t *k_out_dev, int64_t k_stride, uint16_t *v_out_dev, int64_t v_stride, void *hip_stream);
+
+/* Attention of one new token per sequence over its cached tokens (its own among them, once et_kv_append has stored it):
+ *   out[b, h] = sum over t of softmax_t(scale * q[b, h] . k[t, h'])  v[t, h'],   h' = h / (n_heads / n_kv_heads),
+ * t running over the last `window` positions below kv_len[b] (window = 0: all of them) that have a page.  A head
+ * that no token is left for, or whose logits are all minus infinity, gets zeros.  q_dev bf16 [n_seqs, n_heads *
+ * head_dim] with row stride q_stride (a multiple of 8; aligned to 16 bytes); out_dev bf16 [n_seqs, n_heads * head_dim],
+ * contiguous, not q_dev.  max_len: a bound of every kv_len that the host knows (positions from max_len on are left out); it decides how the
+ * work is split, a generous one costs little.  Two equal calls give equal bits.  workspace: et_attention_paged_workspace_bytes
+ * with the same arguments, contents arbitrary; calls that run at the same time need one each.  Asynchronous on `hip_stream`.
+ * Errors: INVALID_ARG, UNSUPPORTED (page_size, head_dim), WORKSPACE, HIP. */
+size_t et_attention_paged_workspace_bytes(const et_kv_cache *cache, const et_kv_seqs *seqs, int32_t n_heads,
+                                          int32_t max_len, int32_t window);
+int et_attention_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, const uint16_t *q_dev, int64_t q_stride,
+                       int32_t n_heads, int32_t max_len, int32_t window, float scale, void *workspace_dev,
+                       size_t workspace_bytes, uint16_t *out_dev, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -13,5 +13,5 @@ from .binding import (  # noqa: F401
     et_encoder_block_qkv,
     et_encoder_create, et_encoder_destroy, et_workspace_bytes, et_encode_clip,
     et_profile_enable, et_profile_read, et_kernel_name, et_merge_profile_enable, et_merge_profile_read,
-    Encoder, Projector, KERNEL_KINDS,
+    et_kv_page_bytes, Encoder, Projector, KVCache, KERNEL_KINDS,
 )

@@ -1,4 +1,5 @@
 """ctypes binding of include/earlytom.h.  Argument marshalling only."""
+import contextlib
 import ctypes as C
 import math
 import os
@@ -55,9 +56,20 @@ class _PlanOut(C.Structure):
                 ("frame_dynamic_dev", C.c_void_p), ("n_segments", C.c_int32)]
 
 
+class _KvCache(C.Structure):
+    _fields_ = [("data_dev", C.c_void_p)] + [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim",
+                                                                       "format")]
+
+
+class _KvSeqs(C.Structure):
+    _fields_ = [("page_table_dev", C.c_void_p), ("table_stride", C.c_int32), ("pages_per_seq", C.c_int32),
+                ("kv_len_dev", C.c_void_p), ("n_seqs", C.c_int32)]
+
+
 ET_MERGE_MEAN, ET_MERGE_ALG1 = 0, 1
 ET_SELECT_UNIFORM, ET_SELECT_DECOUPLED = 0, 1
 ET_SCORE_L2NORM, ET_SCORE_ATTENTION = 0, 1
+ET_KV_BF16, ET_KV_E4M3, ET_KV_INT8 = 0, 1, 2
 
 
 def library_path():
@@ -73,7 +85,7 @@ def load_library():
         raise ImportError("libearlytom.so is not built: run `python -c 'import __graft_entry__ as g; "
                           "g.build()'` (or python paper_2605_30010_amd/build.py) first")
     lib = C.CDLL(_LIB_PATH)
-    i32, f32, vp, sz = C.c_int32, C.c_float, C.c_void_p, C.c_size_t
+    i32, i64, f32, vp, sz = C.c_int32, C.c_int64, C.c_float, C.c_void_p, C.c_size_t
     sig = {
         "et_last_error": (C.c_char_p, []),
         "et_keep_count": (i32, [i32, f32]),
@@ -109,6 +121,11 @@ def load_library():
         "et_projector_destroy": (None, [vp]),
         "et_projector_workspace_bytes": (sz, [vp, i32]),
         "et_project_tokens": (C.c_int, [vp, vp, i32, vp, sz, vp, vp]),
+        "et_kv_page_bytes": (sz, [i32, i32, i32, i32]),
+        "et_kv_append": (C.c_int, [C.POINTER(_KvCache), C.POINTER(_KvSeqs), vp, i32, vp, i64, vp, i64, vp]),
+        "et_kv_read": (C.c_int, [C.POINTER(_KvCache), C.POINTER(_KvSeqs), vp, i32, vp, i64, vp, i64, vp]),
+        "et_attention_paged_workspace_bytes": (sz, [C.POINTER(_KvCache), C.POINTER(_KvSeqs), i32, i32, i32]),
+        "et_attention_paged": (C.c_int, [C.POINTER(_KvCache), C.POINTER(_KvSeqs), vp, i64, i32, i32, i32, f32, vp, sz, vp, vp]),
         "et_merge_profile_enable": (C.c_int, [i32]),
         "et_merge_profile_read": (C.c_int, [C.POINTER(C.c_double), C.POINTER(C.c_int64), C.POINTER(C.c_double),
                                            C.POINTER(C.c_int64), i32]),
@@ -547,6 +564,136 @@ class Projector:
             self.close()
         except Exception:
             pass
+
+
+_KV_FORMATS = {"bf16": ET_KV_BF16, "e4m3": ET_KV_E4M3, "int8": ET_KV_INT8}
+
+
+def et_kv_page_bytes(page_size, n_kv_heads, head_dim, fmt):
+    return int(load_library().et_kv_page_bytes(int(page_size), int(n_kv_heads), int(head_dim), _KV_FORMATS[fmt]))
+
+
+class KVCache:
+    """A paged key-value cache: `data` uint8 [n_pages, page bytes] on the device (layout in earlytom.h), allocated here unless
+    given.  fmt: "bf16", "e4m3" or "int8".  The sequences are the caller's: page_table int32 [n_seqs, pages] (entries outside
+    [0, n_pages) = no page; rows may be strided), kv_len int32 [n_seqs].  Every call is asynchronous on `stream` (default: the
+    current stream of the cache's device), allocates with torch's allocator only, keeps nothing, and can be captured into a
+    graph; calls on several streams may run at the same time as long as none of them stores what another one reads."""
+
+    def __init__(self, n_pages, page_size, n_kv_heads, head_dim, fmt="bf16", data=None, device="cuda:0"):
+        if fmt not in _KV_FORMATS:
+            raise ValueError("fmt must be one of %s" % ", ".join(_KV_FORMATS))
+        size = et_kv_page_bytes(page_size, n_kv_heads, head_dim, fmt)
+        if size == 0 or n_pages < 1:
+            raise ValueError("no such cache: n_pages %d, page_size %d (16, 32, 64, 128, 256), n_kv_heads %d, head_dim %d "
+                             "(64, 80, 96, 128, 256)" % (n_pages, page_size, n_kv_heads, head_dim))
+        if data is None:
+            data = torch.empty((n_pages, size), dtype=torch.uint8, device=device)
+        _dev(data, torch.uint8, "data")
+        if data.numel() != n_pages * size:
+            raise ValueError("data has %d bytes, %d pages of %d are asked for" % (data.numel(), n_pages, size))
+        self.data, self.device, self.fmt = data, data.device, fmt
+        self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = int(n_pages), int(page_size), int(n_kv_heads), int(head_dim)
+        self._cache = _KvCache(data.data_ptr(), self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, _KV_FORMATS[fmt])
+
+    def append(self, k, v, page_table, kv_len, cu_rows=None, stream=None):
+        """Stores rows k, v (bf16 [rows, n_kv_heads * head_dim] or [rows, n_kv_heads, head_dim], rows may be strided) as the last
+        tokens of their sequences; kv_len counts them.  cu_rows int32 [n_seqs + 1]; None: one row for each sequence."""
+        k, v = self._rows(k, "k", self.n_kv_heads), self._rows(v, "v", self.n_kv_heads)
+        if k.shape[0] != v.shape[0]:
+            raise ValueError("k has %d rows, v %d" % (k.shape[0], v.shape[0]))
+        seqs, cu = self._seqs(page_table, kv_len), self._cu(cu_rows, kv_len)
+        with self._on(stream) as s:
+            _check(load_library().et_kv_append(C.byref(self._cache), C.byref(seqs), cu, k.shape[0], k.data_ptr(), k.stride(0),
+                                               v.data_ptr(), v.stride(0), s))
+
+    def read(self, page_table, kv_len, cu_rows=None, rows=None, out=None, stream=None):
+        """The last cu_rows[b + 1] - cu_rows[b] tokens of every sequence b (None: one each) as bf16 rows (k, v), [rows,
+        n_kv_heads * head_dim] each.  Rows that belong to no sequence stay as `out` = (k, v) has them."""
+        seqs, cu = self._seqs(page_table, kv_len), self._cu(cu_rows, kv_len)
+        rows = seqs.n_seqs if rows is None else int(rows)
+        with self._on(stream) as s:
+            if out is None:
+                shape = (max(rows, 0), self.n_kv_heads * self.head_dim)
+                out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=self.device) for _ in range(2))
+            k, v = self._rows(out[0], "out[0]", self.n_kv_heads), self._rows(out[1], "out[1]", self.n_kv_heads)
+            if k.shape[0] < rows or v.shape[0] < rows:
+                raise ValueError("out has fewer than %d rows" % rows)
+            _check(load_library().et_kv_read(C.byref(self._cache), C.byref(seqs), cu, rows, k.data_ptr(), k.stride(0),
+                                             v.data_ptr(), v.stride(0), s))
+        return out
+
+    def attend(self, q, page_table, kv_len, max_len, window=0, scale=None, out=None, stream=None):
+        """Attention of one new token per sequence: q bf16 [n_seqs, n_heads * head_dim] or [n_seqs, n_heads, head_dim] (rows may
+        be strided) -> bf16 [n_seqs, n_heads * head_dim].  max_len: a bound of all kv_len; window: the last so many tokens
+        only (0 = all); scale: default 1 / sqrt(head_dim)."""
+        q = self._rows(q, "q", None)
+        seqs = self._seqs(page_table, kv_len)
+        if q.shape[0] != seqs.n_seqs:
+            raise ValueError("q has %d rows for %d sequences" % (q.shape[0], seqs.n_seqs))
+        heads = q.shape[1] // self.head_dim
+        scale = 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale)
+        lib = load_library()
+        with self._on(stream) as s:
+            if out is None:
+                out = torch.empty((q.shape[0], q.shape[1]), dtype=torch.bfloat16, device=self.device)
+            elif _dev(out, torch.bfloat16, "out").numel() != q.shape[0] * q.shape[1] or out.device != self.device:
+                raise ValueError("out must hold [%d, %d] values on %s" % (q.shape[0], q.shape[1], self.device))
+            need = lib.et_attention_paged_workspace_bytes(C.byref(self._cache), C.byref(seqs), heads, int(max_len), int(window))
+            ws = torch.empty((need,), dtype=torch.uint8, device=self.device) if need else None
+            _check(lib.et_attention_paged(C.byref(self._cache), C.byref(seqs), q.data_ptr(), q.stride(0), heads, int(max_len),
+                                          int(window), scale, None if ws is None else ws.data_ptr(), need, out.data_ptr(), s))
+        return out
+
+    def _rows(self, t, name, heads):
+        """t as [rows, heads * head_dim] with unit column stride."""
+        if not (isinstance(t, torch.Tensor) and t.dtype == torch.bfloat16 and t.device == self.device):
+            raise TypeError("%s must be a bfloat16 tensor on %s" % (name, self.device))
+        if t.dim() == 3 and t.shape[2] == self.head_dim and (t.stride(1) == self.head_dim or t.shape[1] == 1):
+            t = t.as_strided((t.shape[0], t.shape[1] * t.shape[2]), (t.stride(0), t.stride(2)))
+        width = None if heads is None else heads * self.head_dim
+        if t.dim() != 2 or t.stride(1) != 1 or t.shape[1] % self.head_dim or (width is not None and t.shape[1] != width):
+            raise ValueError("%s must be [rows, %s * head_dim] or [rows, %s, head_dim] with contiguous rows"
+                             % (name, heads or "n_heads", heads or "n_heads"))
+        if t.shape[0] <= 1 and t.stride(0) < t.shape[1]:       # the stride of a single row says nothing
+            t = t.as_strided(t.shape, (t.shape[1], 1))
+        return t
+
+    def _seqs(self, page_table, kv_len):
+        for t, name in ((page_table, "page_table"), (kv_len, "kv_len")):
+            if not (isinstance(t, torch.Tensor) and t.dtype == torch.int32 and t.device == self.device):
+                raise TypeError("%s must be an int32 tensor on %s" % (name, self.device))
+        if page_table.dim() != 2 or page_table.shape[1] < 1 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError("page_table must be [n_seqs, pages] with contiguous rows")
+        if kv_len.dim() != 1 or kv_len.shape[0] != page_table.shape[0] or not kv_len.is_contiguous():
+            raise ValueError("kv_len must be contiguous, one for each row of page_table")
+        n, pages = page_table.shape
+        return _KvSeqs(page_table.data_ptr(), max(page_table.stride(0), pages) if n <= 1 else page_table.stride(0), pages,
+                       kv_len.data_ptr(), n)
+
+    def _cu(self, cu_rows, kv_len):
+        if cu_rows is None:
+            return None
+        if not (isinstance(cu_rows, torch.Tensor) and cu_rows.dtype == torch.int32 and cu_rows.device == self.device):
+            raise TypeError("cu_rows must be an int32 tensor on %s" % self.device)
+        if cu_rows.dim() != 1 or cu_rows.shape[0] != kv_len.shape[0] + 1 or not cu_rows.is_contiguous():
+            raise ValueError("cu_rows must be contiguous, one more than there are sequences")
+        return cu_rows.data_ptr()
+
+    @contextlib.contextmanager
+    def _on(self, stream):
+        """The device and the stream of a call, current while it allocates and launches."""
+        if stream is None:
+            if torch.cuda.current_device() == self.device.index:
+                yield torch.cuda.current_stream(self.device).cuda_stream
+            else:
+                with torch.cuda.device(self.device):
+                    yield torch.cuda.current_stream(self.device).cuda_stream
+        else:
+            if stream.device != self.device:
+                raise ValueError("the stream is on %s, the cache on %s" % (stream.device, self.device))
+            with torch.cuda.stream(stream):
+                yield stream.cuda_stream
 
 
 class Encoder:
