@@ -371,7 +371,7 @@ typedef struct {
 } et_kv_cache;
 typedef struct {
   const int32_t *page_table_dev; /* [n_seqs, table_stride], of which pages_per_seq columns are used  */
-  int32_t table_stride, pages_per_seq;
+  int32_t table_stride, pages_per_seq; /* pages_per_seq * page_size at most 2^30                     */
   const int32_t *kv_len_dev; /* [n_seqs]                                                             */
   int32_t n_seqs;
 } et_kv_seqs;

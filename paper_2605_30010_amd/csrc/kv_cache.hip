@@ -169,8 +169,8 @@ int check_kv(const et_kv_cache *c, const et_kv_seqs *s) {
   }
   ET_REQUIRE(c->data_dev != nullptr && (uintptr_t)c->data_dev % 16 == 0, "data_dev of the cache is NULL or not aligned to 16 bytes");
   ET_REQUIRE(s->n_seqs >= 0, "n_seqs = %d is negative", s->n_seqs);
-  ET_REQUIRE(s->pages_per_seq >= 1 && s->table_stride >= s->pages_per_seq && (int64_t)s->pages_per_seq * c->page_size <= INT32_MAX,
-             "pages_per_seq = %d must be at least 1, at most table_stride = %d, and below 2^31 tokens", s->pages_per_seq, s->table_stride);
+  ET_REQUIRE(s->pages_per_seq >= 1 && s->table_stride >= s->pages_per_seq && (int64_t)s->pages_per_seq * c->page_size <= 1 << 30,
+             "pages_per_seq = %d must be at least 1, at most table_stride = %d, and at most 2^30 tokens", s->pages_per_seq, s->table_stride);
   ET_REQUIRE(s->n_seqs == 0 || (s->page_table_dev && s->kv_len_dev), "page_table_dev or kv_len_dev is NULL");
   return ET_OK;
 }
