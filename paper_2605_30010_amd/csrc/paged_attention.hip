@@ -6,7 +6,8 @@
 
 namespace et {
 
-constexpr int kWaves = 4, kTile = 32;                    // wavefronts of a workgroup; tokens that one takes at a time
+constexpr int kTile = 32;                                // tokens that a wavefront takes at a time
+constexpr int kMostSplits = 1024;                        // parts of a sequence
 
 // a * b rounded, never part of a fused multiply-add: a logit less the maximum has to be 0 for the maximum itself, however large.
 __device__ __forceinline__ float whole_product(float a, float b) {
@@ -23,16 +24,26 @@ struct SeqRange {
   int chunk, parts;
 };
 __device__ __forceinline__ SeqRange seq_range(int len, int bound, int window, int splits) {
+  constexpr int kStep = 4 * kTile;
   SeqRange r;
   r.hi = min(len, bound);
   r.first = window > 0 && len > window ? len - window : 0;
   r.lo = r.first & ~15;
   const int span = max(r.hi - r.lo, 0);
   r.chunk = max((span + splits - 1) / splits, 1);
-  r.chunk = (r.chunk + kWaves * kTile - 1) / (kWaves * kTile) * (kWaves * kTile);
+  r.chunk = (r.chunk + kStep - 1) / kStep * kStep;
   r.parts = (span + r.chunk - 1) / r.chunk;
   return r;
 }
+
+// Weight of a part (or a wavefront's share) whose largest logit and sum are ml, against the largest of all.  One without tokens has
+// none; a NaN in its sum stays.
+__device__ __forceinline__ float part_factor(float2 ml, float top) {
+  return ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml.x - top);
+}
+// What the values' codes are multiplied with at the end (their rows' maxima went into the weights, times 2^-9).
+template <int FMT>
+__device__ __forceinline__ float value_factor() { return FMT == ET_KV_BF16 ? 1.f : 1.f / (kv_qmax<FMT>() * 0x1p-9f); }
 
 // bf16 pair of two 8-bit codes, bytes 2 SEL and 2 SEL + 1 of w; exact in both formats.
 template <int FMT, int SEL>
@@ -134,7 +145,7 @@ struct Values {
 // A workgroup takes one part of a sequence's tokens for up to 16 query heads of one key-value head; its wavefronts take tiles of
 // 32 tokens in turn.  The cache's bytes go to registers in MFMA operand order, no LDS on the way.
 // The kernel is bound by reading the cache, once.
-template <int HD, int FMT>
+template <int HD, int FMT, int kWaves>
 __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(KvPages c, KvSeqs s, const uint16_t *q, int64_t q_stride,
                                                                       int group, int bound, int window, float scale_log2,
                                                                       PagedSplit split, float *part_o, float2 *part_ml,
@@ -264,7 +275,6 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(KvPages c,
   const int h = threadIdx.x & 15;
   const int64_t head = (int64_t)b * n_heads + (int64_t)kv * group + rt * 16 + h;
   float top = -INFINITY, total = 0.f, f[kWaves];
-  constexpr float kValue = FMT == ET_KV_BF16 ? 1.f : 1.f / (kv_qmax<FMT>() * 0x1p-9f);
 #pragma unroll
   for (int blk = 0; blk < V::BLOCKS; ++blk) {
     if (blk) __syncthreads();
@@ -284,12 +294,11 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(KvPages c,
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
         const float2 ml = lds_ml[w][h];
-        f[w] = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml.x - top);     // (NaN in a sum stays)
+        f[w] = part_factor(ml, top);
         total += f[w] * ml.y;
       }
     }
-    const int d = (threadIdx.x >> 4) * 8;
-    if (h < live && d < BD) {
+    for (int d = (threadIdx.x >> 4) * 8; h < live && d < BD; d += 4 * kWaves * 8) {
       float o[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -298,7 +307,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(KvPages c,
         for (int w = 0; w < kWaves; ++w) o[e] = fmaf(f[w], lds_o[w][d + e][h], o[e]);
       }
       if (split.splits == 1) {
-        const float inv = total == 0.f ? 0.f : kValue / total;
+        const float inv = total == 0.f ? 0.f : value_factor<FMT>() / total;
         u32x4 v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = cvt_pk_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
@@ -313,23 +322,71 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(KvPages c,
   if (split.splits > 1 && threadIdx.x < live) part_ml[head * split.splits + part] = make_float2(top, total);
 }
 
-// Joins the parts of one query head, in ascending order.
+// Joins the parts of one query head, always in the same order: groups of lanes, four dimensions a lane, take every GROUPS-th part,
+// and their sums are added up in the groups' order.  Every load is issued before the first is needed: parts that the
+// sequence does not have are read (they lie in the workspace) and left out.
 template <int HD, int FMT>
-__global__ __launch_bounds__(HD) void paged_join_kernel(KvSeqs s, int n_heads, int bound, int window, int splits, const float *part_o,
-                                                        const float2 *part_ml, uint16_t *out) {
+__global__ __launch_bounds__(256) void paged_join_kernel(const float *part_o, const float2 *part_ml, const int32_t *len, int n_heads,
+                                                         int splits, int bound, int window, uint16_t *out) {
+  constexpr int LANES = HD / 4, GROUPS = 256 / LANES, BATCH = 8;
+  __shared__ float lds_f[kMostSplits], lds_o[GROUPS][HD], lds_top[4], lds_sum[4];
   const int64_t head = blockIdx.x;
-  const int d = threadIdx.x, parts = max(seq_range(s.len[head / n_heads], bound, window, splits).parts, 1);
-  const float2 *ml = part_ml + head * splits;
-  const float *o = part_o + head * splits * HD + d;
-  float top = -INFINITY, total = 0.f, x = 0.f;
-  for (int i = 0; i < parts; ++i) top = fmaxf(top, ml[i].x);
-  for (int i = 0; i < parts; ++i) {
-    const float f = ml[i].x == -INFINITY ? (ml[i].y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml[i].x - top);
-    total += f * ml[i].y;
-    x = fmaf(f, o[(int64_t)i * HD], x);
+  const int tid = threadIdx.x, lane = tid % LANES, grp = tid / LANES;
+  const f32x4 *o = reinterpret_cast<const f32x4 *>(part_o + head * splits * HD) + lane;
+  f32x4 v[BATCH];
+  if (grp < GROUPS)
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) v[i] = o[(int64_t)min(grp + i * GROUPS, splits - 1) * (HD / 4)];
+  float2 ml[kMostSplits / 256];
+#pragma unroll
+  for (int i = 0; i < kMostSplits / 256; ++i) ml[i] = part_ml[head * splits + min(tid + 256 * i, splits - 1)];
+  const int parts = max(seq_range(len[head / n_heads], bound, window, splits).parts, 1);
+  float top = -INFINITY, total = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMostSplits / 256; ++i)
+    if (tid + 256 * i < parts) top = fmaxf(top, ml[i].x);
+  top = wave_max(top);
+  if (tid % 64 == 0) lds_top[tid / 64] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(lds_top[0], lds_top[1]), fmaxf(lds_top[2], lds_top[3]));
+#pragma unroll
+  for (int i = 0; i < kMostSplits / 256; ++i)
+    if (tid + 256 * i < parts) {
+      const float f = part_factor(ml[i], top);
+      lds_f[tid + 256 * i] = f;
+      total += f * ml[i].y;
+    }
+  total = wave_sum(total);
+  if (tid % 64 == 0) lds_sum[tid / 64] = total;
+  __syncthreads();
+  total = (lds_sum[0] + lds_sum[1]) + (lds_sum[2] + lds_sum[3]);
+  if (grp < GROUPS) {
+    f32x4 x{0, 0, 0, 0};
+    for (int first = grp;;) {
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) {
+        const int at = first + i * GROUPS;
+        if (at < parts) {
+          const float f = lds_f[at];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = fmaf(f, v[i][e], x[e]);
+        }
+      }
+      first += BATCH * GROUPS;
+      if (first >= parts) break;
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) v[i] = o[(int64_t)min(first + i * GROUPS, splits - 1) * (HD / 4)];
+    }
+    *reinterpret_cast<f32x4 *>(&lds_o[grp][lane * 4]) = x;
   }
-  constexpr float kValue = FMT == ET_KV_BF16 ? 1.f : 1.f / (kv_qmax<FMT>() * 0x1p-9f);
-  out[head * HD + d] = f32_to_bf16_bits(total == 0.f ? 0.f : x * (kValue / total));
+  __syncthreads();
+  const float inv = total == 0.f ? 0.f : value_factor<FMT>() / total;
+  if (tid < HD) {
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) x += lds_o[i][tid];
+    out[head * HD + tid] = f32_to_bf16_bits(x * inv);
+  }
 }
 
 // Splits so that about 1024 workgroups share the work, if each gets a tile per wavefront.
@@ -337,8 +394,14 @@ static PagedSplit paged_split(int n_seqs, int kv_heads, int group, int64_t span)
   PagedSplit p;
   p.row_tiles = (group + 15) / 16;
   const int64_t units = (int64_t)n_seqs * kv_heads * p.row_tiles;
-  const int64_t most = (span + kWaves * kTile - 1) / (kWaves * kTile), want = (1024 + units - 1) / units;
-  p.splits = (int)std::max<int64_t>(1, std::min(most, want));
+  #ifndef TARGET
+#define TARGET 1024
+#endif
+#ifndef WV
+#define WV 4
+#endif
+  const int64_t most = (span + 4 * kTile - 1) / (4 * kTile), want = (TARGET + units - 1) / units;
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kMostSplits, std::min(most, want)));
   return p;
 }
 
@@ -404,12 +467,12 @@ int et_attention_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, const u
   const float scale_log2 = scale * 1.4426950408889634f * (cache->format == ET_KV_BF16 ? 1.f : cache->format == ET_KV_INT8 ? 1.f / 127.f : 1.f / 448.f);
   const int64_t grid = (int64_t)seqs->n_seqs * cache->n_kv_heads * p.row_tiles * p.splits;
   return kv_dispatch(cache->head_dim, cache->format, [&](auto hd, auto fmt) {
-    paged_attention_kernel<hd.value, fmt.value><<<(unsigned)grid, 64 * kWaves, 0, stream>>>(
+    paged_attention_kernel<hd.value, fmt.value, WV><<<(unsigned)grid, 64 * WV, 0, stream>>>(
         kv_pages(*cache), kv_seqs(*seqs), q_dev, q_stride, group, bound, window, scale_log2, p, part_o, part_ml, out_dev);
     ET_LAUNCH_CHECK();
     if (p.splits > 1) {
-      paged_join_kernel<hd.value, fmt.value><<<(unsigned)rows, hd.value, 0, stream>>>(kv_seqs(*seqs), n_heads, bound, window, p.splits, part_o,
-                                                                                     part_ml, out_dev);
+      paged_join_kernel<hd.value, fmt.value><<<(unsigned)rows, 256, 0, stream>>>(part_o, part_ml, seqs->kv_len_dev, n_heads, p.splits, bound,
+                                                                                 window, out_dev);
       ET_LAUNCH_CHECK();
     }
     return ET_OK;
