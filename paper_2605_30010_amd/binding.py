@@ -1,5 +1,4 @@
 """ctypes binding of include/earlytom.h.  Argument marshalling only."""
-import contextlib
 import ctypes as C
 import math
 import os
@@ -566,6 +565,9 @@ class Projector:
             pass
 
 
+# The current stream's handle without an object around it (2 us a call less).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
 _KV_FORMATS = {"bf16": ET_KV_BF16, "e4m3": ET_KV_E4M3, "int8": ET_KV_INT8}
 
 
@@ -595,105 +597,113 @@ class KVCache:
         self.data, self.device, self.fmt = data, data.device, fmt
         self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = int(n_pages), int(page_size), int(n_kv_heads), int(head_dim)
         self._cache = _KvCache(data.data_ptr(), self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, _KV_FORMATS[fmt])
+        self._lib, self._width, self._scale = load_library(), self.n_kv_heads * self.head_dim, 1.0 / math.sqrt(self.head_dim)
 
     def append(self, k, v, page_table, kv_len, cu_rows=None, stream=None):
         """Stores rows k, v (bf16 [rows, n_kv_heads * head_dim] or [rows, n_kv_heads, head_dim], rows may be strided) as the last
         tokens of their sequences; kv_len counts them.  cu_rows int32 [n_seqs + 1]; None: one row for each sequence."""
-        k, v = self._rows(k, "k", self.n_kv_heads), self._rows(v, "v", self.n_kv_heads)
-        if k.shape[0] != v.shape[0]:
-            raise ValueError("k has %d rows, v %d" % (k.shape[0], v.shape[0]))
-        seqs, cu = self._seqs(page_table, kv_len), self._cu(cu_rows, kv_len)
-        with self._on(stream) as s:
-            _check(load_library().et_kv_append(C.byref(self._cache), C.byref(seqs), cu, k.shape[0], k.data_ptr(), k.stride(0),
-                                               v.data_ptr(), v.stride(0), s))
+        s = self._here(stream)
+        if s is None:
+            with self._elsewhere(stream):
+                return self.append(k, v, page_table, kv_len, cu_rows)
+        k, v = self._rows(k, "k", self._width), self._rows(v, "v", self._width)
+        rows = k.shape[0]
+        if v.shape[0] != rows:
+            raise ValueError("k has %d rows, v %d" % (rows, v.shape[0]))
+        _check(self._lib.et_kv_append(self._cache, self._seqs(page_table, kv_len), self._cu(cu_rows, kv_len), rows, k.data_ptr(),
+                                      self._stride(k), v.data_ptr(), self._stride(v), s))
 
     def read(self, page_table, kv_len, cu_rows=None, rows=None, out=None, stream=None):
         """The last cu_rows[b + 1] - cu_rows[b] tokens of every sequence b (None: one each) as bf16 rows (k, v), [rows,
         n_kv_heads * head_dim] each.  Rows that belong to no sequence stay as `out` = (k, v) has them."""
+        s = self._here(stream)
+        if s is None:
+            with self._elsewhere(stream):
+                return self.read(page_table, kv_len, cu_rows, rows, out)
         seqs, cu = self._seqs(page_table, kv_len), self._cu(cu_rows, kv_len)
-        rows = seqs.n_seqs if rows is None else int(rows)
-        with self._on(stream) as s:
-            if out is None:
-                shape = (max(rows, 0), self.n_kv_heads * self.head_dim)
-                out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=self.device) for _ in range(2))
-            k, v = self._rows(out[0], "out[0]", self.n_kv_heads), self._rows(out[1], "out[1]", self.n_kv_heads)
+        rows = kv_len.shape[0] if rows is None else int(rows)
+        if out is None:
+            k, v = (torch.empty((max(rows, 0), self._width), dtype=torch.bfloat16, device=self.device) for _ in range(2))
+            out = k, v
+        else:
+            k, v = self._rows(out[0], "out[0]", self._width), self._rows(out[1], "out[1]", self._width)
             if k.shape[0] < rows or v.shape[0] < rows:
                 raise ValueError("out has fewer than %d rows" % rows)
-            _check(load_library().et_kv_read(C.byref(self._cache), C.byref(seqs), cu, rows, k.data_ptr(), k.stride(0),
-                                             v.data_ptr(), v.stride(0), s))
+        _check(self._lib.et_kv_read(self._cache, seqs, cu, rows, k.data_ptr(), self._stride(k), v.data_ptr(), self._stride(v), s))
         return out
 
     def attend(self, q, page_table, kv_len, max_len, window=0, scale=None, out=None, stream=None):
         """Attention of one new token per sequence: q bf16 [n_seqs, n_heads * head_dim] or [n_seqs, n_heads, head_dim] (rows may
         be strided) -> bf16 [n_seqs, n_heads * head_dim].  max_len: a bound of all kv_len; window: the last so many tokens
         only (0 = all); scale: default 1 / sqrt(head_dim)."""
-        q = self._rows(q, "q", None)
-        seqs = self._seqs(page_table, kv_len)
-        if q.shape[0] != seqs.n_seqs:
-            raise ValueError("q has %d rows for %d sequences" % (q.shape[0], seqs.n_seqs))
-        heads = q.shape[1] // self.head_dim
-        scale = 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale)
-        lib = load_library()
-        with self._on(stream) as s:
-            if out is None:
-                out = torch.empty((q.shape[0], q.shape[1]), dtype=torch.bfloat16, device=self.device)
-            elif _dev(out, torch.bfloat16, "out").numel() != q.shape[0] * q.shape[1] or out.device != self.device:
-                raise ValueError("out must hold [%d, %d] values on %s" % (q.shape[0], q.shape[1], self.device))
-            need = lib.et_attention_paged_workspace_bytes(C.byref(self._cache), C.byref(seqs), heads, int(max_len), int(window))
-            ws = torch.empty((need,), dtype=torch.uint8, device=self.device) if need else None
-            _check(lib.et_attention_paged(C.byref(self._cache), C.byref(seqs), q.data_ptr(), q.stride(0), heads, int(max_len),
-                                          int(window), scale, None if ws is None else ws.data_ptr(), need, out.data_ptr(), s))
+        s = self._here(stream)
+        if s is None:
+            with self._elsewhere(stream):
+                return self.attend(q, page_table, kv_len, max_len, window, scale, out)
+        q, seqs, lib = self._rows(q, "q", 0), self._seqs(page_table, kv_len), self._lib
+        n, width = q.shape
+        if n != kv_len.shape[0]:
+            raise ValueError("q has %d rows for %d sequences" % (n, kv_len.shape[0]))
+        heads, max_len, window = width // self.head_dim, int(max_len), int(window)
+        if out is None:
+            out = torch.empty((n, width), dtype=torch.bfloat16, device=self.device)
+        elif _dev(out, torch.bfloat16, "out").numel() != n * width or out.device != self.device:
+            raise ValueError("out must hold [%d, %d] values on %s" % (n, width, self.device))
+        need = lib.et_attention_paged_workspace_bytes(self._cache, seqs, heads, max_len, window)
+        ws = torch.empty((need,), dtype=torch.uint8, device=self.device).data_ptr() if need else None
+        _check(lib.et_attention_paged(self._cache, seqs, q.data_ptr(), self._stride(q), heads, max_len, window,
+                                      self._scale if scale is None else float(scale), ws, need, out.data_ptr(), s))
         return out
 
-    def _rows(self, t, name, heads):
-        """t as [rows, heads * head_dim] with unit column stride."""
-        if not (isinstance(t, torch.Tensor) and t.dtype == torch.bfloat16 and t.device == self.device):
+    def _rows(self, t, name, width):
+        """t as [rows, columns] with unit column stride (width 0: any number of heads)."""
+        if not (isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.device == self.device):
             raise TypeError("%s must be a bfloat16 tensor on %s" % (name, self.device))
         if t.dim() == 3 and t.shape[2] == self.head_dim and (t.stride(1) == self.head_dim or t.shape[1] == 1):
             t = t.as_strided((t.shape[0], t.shape[1] * t.shape[2]), (t.stride(0), t.stride(2)))
-        width = None if heads is None else heads * self.head_dim
-        if t.dim() != 2 or t.stride(1) != 1 or t.shape[1] % self.head_dim or (width is not None and t.shape[1] != width):
-            raise ValueError("%s must be [rows, %s * head_dim] or [rows, %s, head_dim] with contiguous rows"
-                             % (name, heads or "n_heads", heads or "n_heads"))
-        if t.shape[0] <= 1 and t.stride(0) < t.shape[1]:       # the stride of a single row says nothing
-            t = t.as_strided(t.shape, (t.shape[1], 1))
+        if t.dim() != 2 or t.stride(1) != 1 or t.shape[1] % self.head_dim or (width and t.shape[1] != width):
+            heads = width // self.head_dim or "n_heads"
+            raise ValueError("%s must be [rows, %s * head_dim] or [rows, %s, head_dim] with contiguous rows" % (name, heads, heads))
         return t
+
+    @staticmethod
+    def _stride(t):
+        n, width = t.shape
+        return t.stride(0) if n > 1 else width                        # (the stride of a single row says nothing)
 
     def _seqs(self, page_table, kv_len):
         for t, name in ((page_table, "page_table"), (kv_len, "kv_len")):
-            if not (isinstance(t, torch.Tensor) and t.dtype == torch.int32 and t.device == self.device):
+            if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.device == self.device):
                 raise TypeError("%s must be an int32 tensor on %s" % (name, self.device))
         if page_table.dim() != 2 or page_table.shape[1] < 1 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
             raise ValueError("page_table must be [n_seqs, pages] with contiguous rows")
-        if kv_len.dim() != 1 or kv_len.shape[0] != page_table.shape[0] or not kv_len.is_contiguous():
-            raise ValueError("kv_len must be contiguous, one for each row of page_table")
         n, pages = page_table.shape
-        return _KvSeqs(page_table.data_ptr(), max(page_table.stride(0), pages) if n <= 1 else page_table.stride(0), pages,
-                       kv_len.data_ptr(), n)
+        if kv_len.dim() != 1 or kv_len.shape[0] != n or not kv_len.is_contiguous():
+            raise ValueError("kv_len must be contiguous, one for each row of page_table")
+        return _KvSeqs(page_table.data_ptr(), page_table.stride(0) if n > 1 else pages, pages, kv_len.data_ptr(), n)
 
     def _cu(self, cu_rows, kv_len):
         if cu_rows is None:
             return None
-        if not (isinstance(cu_rows, torch.Tensor) and cu_rows.dtype == torch.int32 and cu_rows.device == self.device):
+        if not (isinstance(cu_rows, torch.Tensor) and cu_rows.dtype is torch.int32 and cu_rows.device == self.device):
             raise TypeError("cu_rows must be an int32 tensor on %s" % self.device)
         if cu_rows.dim() != 1 or cu_rows.shape[0] != kv_len.shape[0] + 1 or not cu_rows.is_contiguous():
             raise ValueError("cu_rows must be contiguous, one more than there are sequences")
         return cu_rows.data_ptr()
 
-    @contextlib.contextmanager
-    def _on(self, stream):
-        """The device and the stream of a call, current while it allocates and launches."""
+    def _here(self, stream):
+        """The stream to launch on, if its device is the current one and no other stream is asked for."""
+        if stream is None and torch.cuda.current_device() == self.device.index:
+            return _raw_stream(self.device.index)
+        return None
+
+    def _elsewhere(self, stream):
+        """Makes the cache's device, and `stream` if given, current: allocations have to be made there too."""
         if stream is None:
-            if torch.cuda.current_device() == self.device.index:
-                yield torch.cuda.current_stream(self.device).cuda_stream
-            else:
-                with torch.cuda.device(self.device):
-                    yield torch.cuda.current_stream(self.device).cuda_stream
-        else:
-            if stream.device != self.device:
-                raise ValueError("the stream is on %s, the cache on %s" % (stream.device, self.device))
-            with torch.cuda.stream(stream):
-                yield stream.cuda_stream
+            return torch.cuda.device(self.device)
+        if stream.device != self.device:
+            raise ValueError("the stream is on %s, the cache on %s" % (stream.device, self.device))
+        return torch.cuda.stream(stream)
 
 
 class Encoder:

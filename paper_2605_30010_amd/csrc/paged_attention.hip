@@ -3,11 +3,14 @@
 
 #include "kv_cache.h"
 #include "mfma_common.h"
+#include "select_common.h"
 
 namespace et {
 
 constexpr int kTile = 32;                                // tokens that a wavefront takes at a time
-constexpr int kMostSplits = 1024;                        // parts of a sequence
+constexpr int kWaves = 4;                                // wavefronts of a workgroup
+constexpr int kBlock = kWaves * kTile;
+constexpr int kShare = 512, kFiner = 4;                  // workgroups that a call is shared out over, and how many times as many at most
 
 // a * b rounded, never part of a fused multiply-add: a logit less the maximum has to be 0 for the maximum itself, however large.
 __device__ __forceinline__ float whole_product(float a, float b) {
@@ -15,25 +18,77 @@ __device__ __forceinline__ float whole_product(float a, float b) {
   return a * b;
 }
 
-// How a call is split.  Each sequence's tokens are shared out over up to `splits` workgroups, at least a tile per wavefront each.
-struct PagedSplit {
-  int splits, row_tiles;                                 // row_tiles: groups of 16 query heads of one key-value head
+// How a call's work is shared out.  The tokens of all sequences, in blocks of kBlock, are dealt out evenly over about `share`
+// workgroups per query-head tile; a workgroup gets up to `per` consecutive blocks of one sequence (a part of it), so that lengths
+// that differ leave no workgroup with more than another.  Only the device knows the lengths: each workgroup finds its part by a
+// scan over them, 64 at a time.  There are at most kFiner share + n_seqs parts, whatever the lengths are.
+struct PagedArgs {
+  const int32_t *len;
+  int n_seqs, bound, window;                             // bound: no position from here on counts
+  int share;                                             // 0: every sequence is one part
 };
+// Tokens [first, hi) of a sequence count; lo = first rounded down to 16.
 struct SeqRange {
-  int lo, hi, first;                                     // tokens [first, hi) count; lo = first rounded down to 16
-  int chunk, parts;
+  int lo, hi, first;
+  __device__ __forceinline__ SeqRange(int len, int bound, int window) {
+    hi = min(len, bound);
+    first = window > 0 && len > window ? len - window : 0;
+    lo = first & ~15;
+  }
+  __device__ __forceinline__ uint32_t blocks() const { return hi > lo ? (uint32_t)(hi - lo + kBlock - 1) / kBlock : 0; }
 };
-__device__ __forceinline__ SeqRange seq_range(int len, int bound, int window, int splits) {
-  constexpr int kStep = 4 * kTile;
-  SeqRange r;
-  r.hi = min(len, bound);
-  r.first = window > 0 && len > window ? len - window : 0;
-  r.lo = r.first & ~15;
-  const int span = max(r.hi - r.lo, 0);
-  r.chunk = max((span + splits - 1) / splits, 1);
-  r.chunk = (r.chunk + kStep - 1) / kStep * kStep;
-  r.parts = (span + r.chunk - 1) / r.chunk;
-  return r;
+// Blocks of a part.  Sequences seldom end with a whole part, so where there are several and the parts are long, shorter ones even
+// out what the last parts leave over.
+__device__ __forceinline__ uint32_t part_blocks(const PagedArgs &a, uint32_t total) {
+  const uint32_t per = max((total + a.share - 1) / a.share, 1u);
+  return a.n_seqs > 1 && per > 8 ? max((per + kFiner - 1) / kFiner, 8u) : per;
+}
+struct Part {
+  int seq, index, count;                                 // the index-th of sequence seq's `count`; seq < 0: none
+  int len;                                               // of the sequence
+  uint32_t per, before;                                  // blocks of a part; parts of the sequences before this one
+};
+// Part number `item`, or (of_seq >= 0) what belongs to that sequence.  The same in all lanes.
+__device__ __forceinline__ Part find_part(const PagedArgs &a, int item, int of_seq) {
+  const int lane = threadIdx.x & 63;
+  Part p{-1, 0, 0, 0, 1, 0};
+  if (a.n_seqs == 1) {                                   // (shorter than the scans, and one user waits for the answer)
+    p.len = a.len[0];
+    const uint32_t blocks = SeqRange(p.len, a.bound, a.window).blocks();
+    p.per = part_blocks(a, blocks);
+    p.count = (blocks + p.per - 1) / p.per;
+    p.index = item;
+    if (of_seq >= 0 || item < p.count) p.seq = 0;
+    return p;
+  }
+  int len = 0, total = 0;
+  uint32_t mine = 0;
+  for (int i = lane; i < a.n_seqs; i += 64) {
+    len = a.len[i];
+    mine = SeqRange(len, a.bound, a.window).blocks();
+    total += mine;
+  }
+  total = __builtin_amdgcn_readlane(wave_inclusive_scan(total), 63);
+  p.per = part_blocks(a, total);
+  for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+    if (a.n_seqs > 64) {
+      len = i0 + lane < a.n_seqs ? a.len[i0 + lane] : 0;
+      mine = SeqRange(len, a.bound, a.window).blocks();
+    }
+    const int parts = (mine + p.per - 1) / p.per, upto = wave_inclusive_scan(parts);
+    const uint64_t found = of_seq < 0 ? __ballot((uint32_t)item < p.before + upto) : of_seq < i0 + 64 ? 1ull << (of_seq & 63) : 0;
+    if (found) {
+      const int at = __builtin_ctzll(found);
+      p.seq = i0 + at;
+      p.len = __builtin_amdgcn_readlane(len, at);
+      p.count = __builtin_amdgcn_readlane(parts, at);
+      p.before += __builtin_amdgcn_readlane(upto, at) - p.count;
+      p.index = item - (int)p.before;
+      return p;
+    }
+    p.before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return p;
 }
 
 // Weight of a part (or a wavefront's share) whose largest logit and sum are ml, against the largest of all.  One without tokens has
@@ -145,11 +200,12 @@ struct Values {
 // A workgroup takes one part of a sequence's tokens for up to 16 query heads of one key-value head; its wavefronts take tiles of
 // 32 tokens in turn.  The cache's bytes go to registers in MFMA operand order, no LDS on the way.
 // The kernel is bound by reading the cache, once.
-template <int HD, int FMT, int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(KvPages c, KvSeqs s, const uint16_t *q, int64_t q_stride,
-                                                                      int group, int bound, int window, float scale_log2,
-                                                                      PagedSplit split, float *part_o, float2 *part_ml,
-                                                                      uint16_t *out) {
+template <int HD, int FMT>
+__global__ __launch_bounds__(64 * kWaves, HD > 128 ? 2 : 3) void paged_attention_kernel(const int32_t *len, const int32_t *table, int n_seqs,
+                                                                      int share, int bound, int window, int units, int row_tiles,
+                                                                      int page_shift, int table_stride, const uint16_t *q, int64_t q_stride,
+                                                                      char *data, int64_t page_bytes, int n_pages, int group, float scale_log2,
+                                                                      float *part_o, float2 *part_ml, uint16_t *out) {
   using Lay = KvLayout<HD, FMT>;
   using K = Keys<HD, FMT>;
   using V = Values<HD, FMT>;
@@ -158,15 +214,57 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(KvPages c,
   __shared__ float lds_o[kWaves][BD][16];
   __shared__ float2 lds_ml[kWaves][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  const int part = blockIdx.x % split.splits, unit = blockIdx.x / split.splits;
-  const int rt = unit % split.row_tiles, kv = unit / split.row_tiles % c.kv_heads, b = unit / (split.row_tiles * c.kv_heads);
-  const int n_heads = group * c.kv_heads, ps = 1 << c.page_shift;
+  const PagedArgs a{len, n_seqs, bound, window, share};
+  const int item = blockIdx.x / units, unit = blockIdx.x % units, rt = unit % row_tiles, kv = unit / row_tiles;
+  const int n_heads = group * (units / row_tiles), ps = 1 << page_shift;
   const int live = min(16, group - rt * 16);              // query heads of this workgroup
-  const SeqRange sr = seq_range(s.len[b], bound, window, split.splits);
-  if (part >= max(sr.parts, 1)) return;
-  const int start = sr.lo + part * sr.chunk, end = min(sr.hi, start + sr.chunk);
+  Part part{item, 0, 1, 0, 0, 0};
+  if (a.share) {
+    part = find_part(a, item, -1);
+    if (part.seq < 0) return;
+  } else {
+    part.len = a.len[item];
+  }
+  const int b = __builtin_amdgcn_readfirstlane(part.seq);
+  const SeqRange sr(part.len, a.bound, a.window);
+  const int start = sr.lo + part.index * (int)part.per * kBlock;
+  const int end = a.share ? (int)min((int64_t)sr.hi, (int64_t)start + (int64_t)part.per * kBlock) : sr.hi;
   const int tiles = end > start ? (end - start + kTile - 1) / kTile : 0;
 
+  f32x4 acc[ACC];
+#pragma unroll
+  for (int j = 0; j < ACC; ++j) acc[j] = f32x4{0, 0, 0, 0};
+  float m = -INFINITY, sum = 0.f;                         // of query head r; sum: this lane's tokens only
+
+  const int32_t *row = table + (int64_t)b * table_stride;
+  int page_of = -1;                                       // lane i: page of the wavefront's i-th group of 16 tokens, of 64
+  auto fetch_pages = [&](int t) {
+    const int pos = start + (t + (lane >> 1) * kWaves) * kTile + (lane & 1) * 16;
+    page_of = pos < end ? row[pos >> page_shift] : -1;
+    if (page_of >= n_pages) page_of = -1;
+  };
+  // (A group without a page reads the first page's bytes, and its tokens do not count.)
+  auto head_of = [&](int page) { return data + max(page, 0) * page_bytes + (int64_t)kv * Lay::head_bytes(ps); };
+  struct Tile {
+    uint32_t kw[2][K::NREG];
+    uint2 km[2], vm[2];
+    int page[2];
+  };
+  auto load_keys = [&](Tile &x, int t, int i) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      x.page[u] = __builtin_amdgcn_readlane(page_of, i + u);
+      const int at = (start + t * kTile + 16 * u) & (ps - 1);
+      const char *head = head_of(x.page[u]);
+      K::load(head + at * Lay::kRow, r, g, x.kw[u]);
+      if constexpr (FMT != ET_KV_BF16) {
+        x.km[u] = *reinterpret_cast<const uint2 *>(head + Lay::key_max(ps) + (at + 4 * g) * 2);
+        x.vm[u] = *reinterpret_cast<const uint2 *>(head + Lay::value_max(ps) + (at + 4 * g) * 2);
+      }
+    }
+  };
+  Tile next;
+  fetch_pages(wave);                                      // (in front of the queries' loads: the keys' wait for it)
   u32x4 qf[K::STEPS];
 #pragma unroll
   for (int st = 0; st < K::STEPS; ++st) {
@@ -175,39 +273,25 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(KvPages c,
     if (r < live && d < HD)
       qf[st] = *reinterpret_cast<const u32x4 *>(q + b * q_stride + ((int64_t)kv * group + rt * 16 + r) * HD + d);
   }
-  f32x4 acc[ACC];
-#pragma unroll
-  for (int j = 0; j < ACC; ++j) acc[j] = f32x4{0, 0, 0, 0};
-  float m = -INFINITY, sum = 0.f;                         // of query head r; sum: this lane's tokens only
-
-  const int32_t *row = s.table + (int64_t)b * s.table_stride;
-  int page_of = -1;                                       // lane i: page of the wavefront's i-th group of 16 tokens, of 64
-  for (int t = wave, i = 0; t < tiles; t += kWaves, i = (i + 2) & 63) {
-    if (i == 0) {
-      const int pos = start + (t + (lane >> 1) * kWaves) * kTile + (lane & 1) * 16;
-      page_of = pos < end ? row[pos >> c.page_shift] : -1;
-      if (page_of >= c.n_pages) page_of = -1;
-    }
+  load_keys(next, wave, 0);
+  for (int t = wave, i = 0; t < tiles; t += kWaves) {
+    const Tile cur = next;
     const int pos0 = start + t * kTile;
-    uint32_t kw[2][K::NREG], vw[V::BLOCKS][8][V::NREG];
-    uint2 km[2], vm[2];
-    int page[2];
+    const uint2 *km = cur.km, *vm = cur.vm;
+    const int *page = cur.page;
+    const auto &kw = cur.kw;
+    uint32_t vw[8][V::NREG];
+    auto load_values = [&](int blk) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      page[u] = __builtin_amdgcn_readlane(page_of, i + u);
-      const int at = (pos0 + 16 * u) & (ps - 1);
-      const char *head = c.data + max(page[u], 0) * c.page_bytes + (int64_t)kv * Lay::head_bytes(ps);
-      K::load(head + at * Lay::kRow, r, g, kw[u]);
-      const char *values = head + Lay::values(ps) + at * Lay::kRow;
+      for (int u = 0; u < 2; ++u) {
+        const char *values = head_of(page[u]) + Lay::values(ps) + ((pos0 + 16 * u) & (ps - 1)) * Lay::kRow;
 #pragma unroll
-      for (int blk = 0; blk < V::BLOCKS; ++blk)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) V::load(values, 4 * g + e, r, blk, vw[blk][4 * u + e]);
-      if constexpr (FMT != ET_KV_BF16) {
-        km[u] = *reinterpret_cast<const uint2 *>(head + Lay::key_max(ps) + (at + 4 * g) * 2);
-        vm[u] = *reinterpret_cast<const uint2 *>(head + Lay::value_max(ps) + (at + 4 * g) * 2);
+        for (int e = 0; e < 4; ++e) V::load(values, 4 * g + e, r, blk, vw[4 * u + e]);
       }
-    }
+    };
+    load_values(0);
+    i = (i + 2) & 63;
+    if (i == 0) fetch_pages(t + kWaves);
     float z[8];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -221,6 +305,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(KvPages c,
         z[4 * u + e] = whole_product(d[e], f);
       }
     }
+    load_keys(next, t + kWaves, i);
     // tokens that do not count: no page, past the end, before the window
     const bool whole = page[0] >= 0 && page[1] >= 0 && pos0 >= sr.first && pos0 + kTile <= end;
     uint32_t dead = 0;
@@ -231,10 +316,6 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(KvPages c,
         if (page[e / 4] < 0 || pos < sr.first || pos >= end) {
           dead |= 1u << e;
           z[e] = -INFINITY;
-#pragma unroll
-          for (int blk = 0; blk < V::BLOCKS; ++blk)
-#pragma unroll
-            for (int x = 0; x < V::NREG; ++x) vw[blk][e][x] = 0;           // (0 times what lies there could be NaN)
         }
       }
     }
@@ -263,9 +344,17 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(KvPages c,
     }
     const u32x4 pf{cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3]), cvt_pk_bf16(p[4], p[5]), cvt_pk_bf16(p[6], p[7])};
 #pragma unroll
-    for (int blk = 0; blk < V::BLOCKS; ++blk)
+    for (int blk = 0; blk < V::BLOCKS; ++blk) {
+      if (!whole) {
 #pragma unroll
-      for (int j = 0; j < V::DPL; ++j) acc[blk * V::DPL + j] = mfma16(V::operand(vw[blk], j), pf, acc[blk * V::DPL + j]);
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int x = 0; x < V::NREG; ++x) vw[e][x] = dead >> e & 1 ? 0 : vw[e][x];     // (0 times what lies there could be NaN)
+      }
+#pragma unroll
+      for (int j = 0; j < V::DPL; ++j) acc[blk * V::DPL + j] = mfma16(V::operand(vw, j), pf, acc[blk * V::DPL + j]);
+      if (blk + 1 < V::BLOCKS) load_values(blk + 1);
+    }
   }
 
   // the wavefronts' results together
@@ -274,6 +363,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(KvPages c,
   if (g == 0) lds_ml[wave][r] = make_float2(m, sum);
   const int h = threadIdx.x & 15;
   const int64_t head = (int64_t)b * n_heads + (int64_t)kv * group + rt * 16 + h;
+  const int64_t slot = (int64_t)item * n_heads + kv * group + rt * 16 + h;       // of a part that is one of several
   float top = -INFINITY, total = 0.f, f[kWaves];
 #pragma unroll
   for (int blk = 0; blk < V::BLOCKS; ++blk) {
@@ -306,112 +396,105 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(KvPages c,
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) o[e] = fmaf(f[w], lds_o[w][d + e][h], o[e]);
       }
-      if (split.splits == 1) {
+      if (part.count == 1) {
         const float inv = total == 0.f ? 0.f : value_factor<FMT>() / total;
         u32x4 v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = cvt_pk_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
         *reinterpret_cast<u32x4 *>(out + head * HD + blk * BD + d) = v;
       } else {
-        float *to = part_o + (head * split.splits + part) * HD + blk * BD + d;
+        float *to = part_o + slot * HD + blk * BD + d;
         *reinterpret_cast<f32x4 *>(to) = f32x4{o[0], o[1], o[2], o[3]};
         *reinterpret_cast<f32x4 *>(to + 4) = f32x4{o[4], o[5], o[6], o[7]};
       }
     }
   }
-  if (split.splits > 1 && threadIdx.x < live) part_ml[head * split.splits + part] = make_float2(top, total);
+  if (part.count > 1 && threadIdx.x < live) part_ml[slot] = make_float2(top, total);
 }
 
 // Joins the parts of one query head, always in the same order: groups of lanes, four dimensions a lane, take every GROUPS-th part,
-// and their sums are added up in the groups' order.  Every load is issued before the first is needed: parts that the
-// sequence does not have are read (they lie in the workspace) and left out.
-template <int HD, int FMT>
-__global__ __launch_bounds__(256) void paged_join_kernel(const float *part_o, const float2 *part_ml, const int32_t *len, int n_heads,
-                                                         int splits, int bound, int window, uint16_t *out) {
-  constexpr int LANES = HD / 4, GROUPS = 256 / LANES, BATCH = 8;
-  __shared__ float lds_f[kMostSplits], lds_o[GROUPS][HD], lds_top[4], lds_sum[4];
-  const int64_t head = blockIdx.x;
+// and their sums are added up in the groups' order; the loads of eight parts of a group are in flight together.  A head whose
+// sequence is one part has its result already.  THREADS: 64 where a sequence has few parts.
+template <int HD, int FMT, int THREADS>
+__global__ __launch_bounds__(THREADS) void paged_join_kernel(const int32_t *len, const float *part_o, const float2 *part_ml, int n_seqs,
+                                                             int share, int bound, int window, int n_heads, uint16_t *out) {
+  constexpr int LANES = HD / 4, GROUPS = THREADS / LANES, BATCH = 8, WAVES = THREADS / 64;
+  __shared__ float lds_o[GROUPS][HD], lds_sum[GROUPS], lds_top[WAVES];
+  const PagedArgs a{len, n_seqs, bound, window, share};
+  const int b = blockIdx.x / n_heads, h = blockIdx.x % n_heads;
   const int tid = threadIdx.x, lane = tid % LANES, grp = tid / LANES;
-  const f32x4 *o = reinterpret_cast<const f32x4 *>(part_o + head * splits * HD) + lane;
   f32x4 v[BATCH];
-  if (grp < GROUPS)
+  float2 s[BATCH];
+  auto load = [&](int before, int first, int last) {
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) v[i] = o[(int64_t)min(grp + i * GROUPS, splits - 1) * (HD / 4)];
-  float2 ml[kMostSplits / 256];
-#pragma unroll
-  for (int i = 0; i < kMostSplits / 256; ++i) ml[i] = part_ml[head * splits + min(tid + 256 * i, splits - 1)];
-  const int parts = max(seq_range(len[head / n_heads], bound, window, splits).parts, 1);
-  float top = -INFINITY, total = 0.f;
-#pragma unroll
-  for (int i = 0; i < kMostSplits / 256; ++i)
-    if (tid + 256 * i < parts) top = fmaxf(top, ml[i].x);
-  top = wave_max(top);
-  if (tid % 64 == 0) lds_top[tid / 64] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(lds_top[0], lds_top[1]), fmaxf(lds_top[2], lds_top[3]));
-#pragma unroll
-  for (int i = 0; i < kMostSplits / 256; ++i)
-    if (tid + 256 * i < parts) {
-      const float f = part_factor(ml[i], top);
-      lds_f[tid + 256 * i] = f;
-      total += f * ml[i].y;
+    for (int i = 0; i < BATCH; ++i) {
+      const int64_t at = (int64_t)(before + min(first + i * GROUPS, last)) * n_heads + h;
+      s[i] = part_ml[at];
+      v[i] = reinterpret_cast<const f32x4 *>(part_o + at * HD)[lane];
     }
-  total = wave_sum(total);
-  if (tid % 64 == 0) lds_sum[tid / 64] = total;
-  __syncthreads();
-  total = (lds_sum[0] + lds_sum[1]) + (lds_sum[2] + lds_sum[3]);
+  };
+  // a single sequence's parts come first, however many there are: their loads need not wait for its length
+  if (n_seqs == 1 && grp < GROUPS) load(0, grp, share - 1);
+  const Part p = find_part(a, 0, b);
+  if (p.count == 1) return;
+  if (n_seqs > 1 && grp < GROUPS && p.count) load(p.before, grp, p.count - 1);
+  const float2 *ml = part_ml + (int64_t)p.before * n_heads + h;
+  float top = -INFINITY;
+  for (int i = tid; i < p.count; i += THREADS) top = fmaxf(top, ml[(int64_t)i * n_heads].x);
+  top = wave_max(top);
+  if constexpr (WAVES > 1) {
+    if (tid % 64 == 0) lds_top[tid / 64] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, lds_top[w]);
+  }
   if (grp < GROUPS) {
     f32x4 x{0, 0, 0, 0};
-    for (int first = grp;;) {
+    float total = 0.f;
+    for (int first = grp; first < p.count; first += BATCH * GROUPS) {
+      if (first != grp) load(p.before, first, p.count - 1);
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        const int at = first + i * GROUPS;
-        if (at < parts) {
-          const float f = lds_f[at];
+      for (int i = 0; i < BATCH; ++i)
+        if (first + i * GROUPS < p.count) {
+          const float f = part_factor(s[i], top);
+          total = fmaf(f, s[i].y, total);
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[e] = fmaf(f, v[i][e], x[e]);
         }
-      }
-      first += BATCH * GROUPS;
-      if (first >= parts) break;
-#pragma unroll
-      for (int i = 0; i < BATCH; ++i) v[i] = o[(int64_t)min(first + i * GROUPS, splits - 1) * (HD / 4)];
     }
     *reinterpret_cast<f32x4 *>(&lds_o[grp][lane * 4]) = x;
+    if (lane == 0) lds_sum[grp] = total;
   }
   __syncthreads();
-  const float inv = total == 0.f ? 0.f : value_factor<FMT>() / total;
-  if (tid < HD) {
-    float x = 0.f;
+  for (int d = tid; d < HD; d += THREADS) {
+    float x = 0.f, total = 0.f;
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) x += lds_o[i][tid];
-    out[head * HD + tid] = f32_to_bf16_bits(x * inv);
+    for (int i = 0; i < GROUPS; ++i) {
+      x += lds_o[i][d];
+      total += lds_sum[i];
+    }
+    out[(int64_t)blockIdx.x * HD + d] = f32_to_bf16_bits(total == 0.f ? 0.f : x * (value_factor<FMT>() / total));
   }
 }
 
-// Splits so that about 1024 workgroups share the work, if each gets a tile per wavefront.
-static PagedSplit paged_split(int n_seqs, int kv_heads, int group, int64_t span) {
-  PagedSplit p;
-  p.row_tiles = (group + 15) / 16;
-  const int64_t units = (int64_t)n_seqs * kv_heads * p.row_tiles;
-  #ifndef TARGET
-#define TARGET 1024
-#endif
-#ifndef WV
-#define WV 4
-#endif
-  const int64_t most = (span + 4 * kTile - 1) / (4 * kTile), want = (TARGET + units - 1) / units;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kMostSplits, std::min(most, want)));
+struct PagedPlan {
+  int group, row_tiles, units, bound, share;
+  int64_t items;                                         // workgroups per unit
+  size_t slots, bytes;                                   // of the workspace
+};
+static PagedPlan paged_plan(const et_kv_cache &c, const et_kv_seqs &s, int n_heads, int max_len, int window) {
+  PagedPlan p;
+  p.group = n_heads / c.n_kv_heads;
+  p.row_tiles = (p.group + 15) / 16;
+  p.units = p.row_tiles * c.n_kv_heads;
+  p.bound = std::min(max_len, s.pages_per_seq * c.page_size);
+  const int span = window > 0 ? (int)std::min<int64_t>(p.bound, (int64_t)window + 15) : p.bound;
+  const int64_t blocks = (int64_t)s.n_seqs * ((span + kBlock - 1) / kBlock);
+  p.share = span <= 4 * kBlock ? 0 : (int)std::min<int64_t>(blocks, (kShare + p.units - 1) / p.units);
+  p.items = p.share * (s.n_seqs > 1 ? kFiner : 1) + (int64_t)s.n_seqs;
+  p.slots = p.share ? (size_t)p.items * n_heads : 0;
+  p.bytes = p.slots * (c.head_dim * sizeof(float) + sizeof(float2));
   return p;
-}
-
-static int64_t paged_span(const et_kv_cache &c, const et_kv_seqs &s, int max_len, int window) {
-  const int64_t bound = std::min<int64_t>(max_len, (int64_t)s.pages_per_seq * c.page_size);
-  return window > 0 ? std::min<int64_t>(bound, (int64_t)window + 15) : bound;
-}
-
-static size_t paged_workspace(int64_t rows, int head_dim, int splits) {
-  return splits == 1 ? 0 : (size_t)rows * splits * (head_dim * sizeof(float) + sizeof(float2));
 }
 
 static int check_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, int n_heads, int max_len, int window) {
@@ -421,8 +504,9 @@ static int check_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, int n_h
              "n_heads = %d must be a multiple of n_kv_heads = %d, at most 65536", n_heads, cache->n_kv_heads);
   ET_REQUIRE(max_len >= 1, "max_len = %d must be at least 1", max_len);
   ET_REQUIRE(window >= 0, "window = %d is negative", window);
-  ET_REQUIRE((int64_t)seqs->n_seqs * n_heads <= INT32_MAX / 1024, "n_seqs * n_heads = %lld is above %d", (long long)seqs->n_seqs * n_heads,
-             INT32_MAX / 1024);
+  ET_REQUIRE((int64_t)seqs->n_seqs * n_heads <= 1 << 24, "n_seqs * n_heads = %lld is above 2^24", (long long)seqs->n_seqs * n_heads);
+  ET_REQUIRE((int64_t)seqs->n_seqs * std::min(max_len, seqs->pages_per_seq * cache->page_size) <= 1ll << 36,
+             "n_seqs * max_len is above 2^36");
   return ET_OK;
 }
 
@@ -435,8 +519,7 @@ extern "C" {
 size_t et_attention_paged_workspace_bytes(const et_kv_cache *cache, const et_kv_seqs *seqs, int32_t n_heads, int32_t max_len,
                                           int32_t window) {
   if (check_paged(cache, seqs, n_heads, max_len, window) || seqs->n_seqs == 0) return 0;
-  const PagedSplit p = paged_split(seqs->n_seqs, cache->n_kv_heads, n_heads / cache->n_kv_heads, paged_span(*cache, *seqs, max_len, window));
-  return paged_workspace((int64_t)seqs->n_seqs * n_heads, cache->head_dim, p.splits);
+  return paged_plan(*cache, *seqs, n_heads, max_len, window).bytes;
 }
 
 int et_attention_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, const uint16_t *q_dev, int64_t q_stride, int32_t n_heads,
@@ -450,29 +533,29 @@ int et_attention_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, const u
              "q_dev or out_dev is NULL or not aligned to 16 bytes");
   ET_REQUIRE(q_stride % 8 == 0 && q_stride >= (int64_t)n_heads * cache->head_dim, "q_stride = %lld must be a multiple of 8 and at least %lld",
              (long long)q_stride, (long long)n_heads * cache->head_dim);
-  const int group = n_heads / cache->n_kv_heads, bound = (int)std::min<int64_t>(max_len, (int64_t)seqs->pages_per_seq * cache->page_size);
-  const PagedSplit p = paged_split(seqs->n_seqs, cache->n_kv_heads, group, paged_span(*cache, *seqs, max_len, window));
-  const int64_t rows = (int64_t)seqs->n_seqs * n_heads;
-  const size_t need = paged_workspace(rows, cache->head_dim, p.splits);
-  if (need) {
+  const PagedPlan p = paged_plan(*cache, *seqs, n_heads, max_len, window);
+  if (p.bytes) {
     ET_REQUIRE(workspace_dev != nullptr && (uintptr_t)workspace_dev % 16 == 0, "workspace_dev is NULL or not aligned to 16 bytes");
-    if (workspace_bytes < need) {
-      set_error("workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, need);
+    if (workspace_bytes < p.bytes) {
+      set_error("workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, p.bytes);
       return ET_ERR_WORKSPACE;
     }
   }
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   float *part_o = static_cast<float *>(workspace_dev);
-  float2 *part_ml = reinterpret_cast<float2 *>(part_o + (need ? rows * p.splits * cache->head_dim : 0));
+  float2 *part_ml = reinterpret_cast<float2 *>(part_o + p.slots * cache->head_dim);
   const float scale_log2 = scale * 1.4426950408889634f * (cache->format == ET_KV_BF16 ? 1.f : cache->format == ET_KV_INT8 ? 1.f / 127.f : 1.f / 448.f);
-  const int64_t grid = (int64_t)seqs->n_seqs * cache->n_kv_heads * p.row_tiles * p.splits;
+  const KvPages c = kv_pages(*cache);
   return kv_dispatch(cache->head_dim, cache->format, [&](auto hd, auto fmt) {
-    paged_attention_kernel<hd.value, fmt.value, WV><<<(unsigned)grid, 64 * WV, 0, stream>>>(
-        kv_pages(*cache), kv_seqs(*seqs), q_dev, q_stride, group, bound, window, scale_log2, p, part_o, part_ml, out_dev);
+    paged_attention_kernel<hd.value, fmt.value><<<(unsigned)(p.items * p.units), 64 * kWaves, 0, stream>>>(
+        seqs->kv_len_dev, seqs->page_table_dev, seqs->n_seqs, p.share, p.bound, window, p.units, p.row_tiles, c.page_shift, seqs->table_stride,
+        q_dev, q_stride, c.data, c.page_bytes, c.n_pages, p.group, scale_log2, part_o, part_ml, out_dev);
     ET_LAUNCH_CHECK();
-    if (p.splits > 1) {
-      paged_join_kernel<hd.value, fmt.value><<<(unsigned)rows, 256, 0, stream>>>(part_o, part_ml, seqs->kv_len_dev, n_heads, p.splits, bound,
-                                                                                 window, out_dev);
+    if (p.share) {
+      const bool few = p.share <= 16 * (int64_t)seqs->n_seqs;
+      const unsigned heads = (unsigned)(seqs->n_seqs * n_heads);
+      (few ? paged_join_kernel<hd.value, fmt.value, 64> : paged_join_kernel<hd.value, fmt.value, 256>)<<<heads, few ? 64 : 256, 0, stream>>>(
+          seqs->kv_len_dev, part_o, part_ml, seqs->n_seqs, p.share, p.bound, window, n_heads, out_dev);
       ET_LAUNCH_CHECK();
     }
     return ET_OK;

@@ -136,3 +136,24 @@ def test_binding_refuses_host_tensors():
         et.KVCache(0, 16, 2, 64)
     with pytest.raises(ValueError):
         et.KVCache(2, 16, 2, 64, fmt="fp8")
+
+
+def test_attention_workspace():
+    """Short sequences need none; the rest as much as is asked for, whatever the bound, and less is refused."""
+    lib = et.load_library()
+    need = lambda c, s, heads, max_len, window: lib.et_attention_paged_workspace_bytes(C.byref(c), C.byref(s), heads, max_len, window)
+    c, long = cache(), seqs(pages_per_seq=1 << 20, table_stride=1 << 20)
+    assert need(c, seqs(), 4, 64, 0) == 0 and need(c, long, 4, 10 ** 6, 64) == 0
+    b = need(c, long, 4, 10 ** 6, 0)
+    assert 0 < b <= 64 << 20 and need(c, long, 4, 2 ** 31 - 1, 0) == b
+    assert need(c, long, 3, 10 ** 6, 0) == 0 and need(c, long, 4, 0, 0) == 0 and need(cache(head_dim=72), long, 4, 10 ** 6, 0) == 0
+    assert attend_call(s=long, max_len=10 ** 6, ws_bytes=b - 1) == -2 and "workspace" in et.et_last_error()
+    assert attend_call(s=long, max_len=10 ** 6, ws_bytes=0) == -2
+    assert attend_call(s=long, max_len=10 ** 6, ws=None) == -1
+    assert attend_call(s=long, max_len=10 ** 6, ws=FAKE + 4) == -1
+
+
+def test_attention_of_too_much_at_once():
+    assert attend_call(s=seqs(n_seqs=1 << 23), heads=4) == -1 and "2^24" in et.et_last_error()
+    assert attend_call(s=seqs(n_seqs=1 << 20, pages_per_seq=1 << 20, table_stride=1 << 20), max_len=10 ** 6) == -1
+    assert "2^36" in et.et_last_error()
