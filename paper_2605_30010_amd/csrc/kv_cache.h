@@ -15,11 +15,6 @@ struct KvPages {
   int32_t n_pages, page_shift;             // tokens per page = 1 << page_shift
   int32_t kv_heads;
 };
-struct KvSeqs {
-  const int32_t *table, *len;
-  int32_t table_stride, pages_per_seq, n_seqs;
-};
-
 // Byte offsets within a head's part of a page.
 template <int HD, int FMT>
 struct KvLayout {
@@ -33,7 +28,6 @@ struct KvLayout {
 
 int check_kv(const et_kv_cache *cache, const et_kv_seqs *seqs);   // ET_OK or an error with its message
 KvPages kv_pages(const et_kv_cache &c);
-KvSeqs kv_seqs(const et_kv_seqs &s);
 
 // Calls f with the head width and the format as constants.
 template <typename F>
