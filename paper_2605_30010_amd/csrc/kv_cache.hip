@@ -152,19 +152,18 @@ __device__ __forceinline__ u32x4 dequantise8(uint2 codes, KvFactor f) {
 constexpr int kBatch = 4;
 template <int HD, int FMT, bool STORE>
 __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const int32_t *len, const int32_t *table, int n_seqs, int rows,
-                                                      int per_block, int table_stride, int pages_per_seq, int n_pages, int page_shift,
-                                                      int kv_heads, char *data, int64_t page_bytes, uint16_t *k, int64_t k_stride,
-                                                      uint16_t *v, int64_t v_stride) {
+                                                      int per_block, int table_stride, int pages_per_seq, int page_shift, KvPages c,
+                                                      uint16_t *k, int64_t k_stride, uint16_t *v, int64_t v_stride) {
   using Lay = KvLayout<HD, FMT>;
   constexpr int LANES = kv_lanes<HD>(), GROUPS = 256 / LANES;
   __shared__ int4 lds_place[64];                         // byte offset of the page (two words), token of the page, 0 / 1 / 2
   const int first = blockIdx.x * per_block, count = min(per_block, rows - first);
   if (threadIdx.x < 64) {
-    const KvPlace p = kv_place(cu, first, count, KvSeqs{table, len, table_stride, pages_per_seq, n_seqs}, n_pages, page_shift);
-    const int64_t page = max(p.page, 0) * page_bytes;
+    const KvPlace p = kv_place(cu, first, count, KvSeqs{table, len, table_stride, pages_per_seq, n_seqs}, c.n_pages, page_shift);
+    const int64_t page = max(p.page, 0) * c.page_bytes;
     lds_place[threadIdx.x] = make_int4((int)page, (int)(page >> 32), p.at, p.owned ? (p.page >= 0 ? 2 : 1) : 0);
   }
-  const int n = 1 << page_shift, sub = threadIdx.x % LANES, heads2 = 2 * kv_heads, head_bytes = Lay::head_bytes(n);
+  const int n = 1 << page_shift, sub = threadIdx.x % LANES, heads2 = 2 * c.kv_heads, head_bytes = Lay::head_bytes(n);
   const int skip = GROUPS / heads2, over = GROUPS % heads2;           // tokens and heads from one turn of a group to its next
   int token = threadIdx.x / LANES / heads2, j = threadIdx.x / LANES % heads2;
   const bool in_row = sub * 8 < HD;
@@ -181,10 +180,10 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const i
     for (int i = 0; i < N; ++i) {
       const int4 place = lds_place[min(token, 63)];
       go[i] = token < count ? place.w : 0;
-      const bool value = j >= kv_heads;
-      const int h = value ? j - kv_heads : j;
+      const bool value = j >= c.kv_heads;
+      const int h = value ? j - c.kv_heads : j;
       row[i] = (value ? v + (first + (int64_t)token) * v_stride : k + (first + (int64_t)token) * k_stride) + h * HD + sub * 8;
-      char *page = data + (int64_t)((uint64_t)(uint32_t)place.y << 32 | (uint32_t)place.x);
+      char *page = c.data + (int64_t)((uint64_t)(uint32_t)place.y << 32 | (uint32_t)place.x);
       const uint32_t head = (uint32_t)h * head_bytes;
       cell[i] = page + (head + (value ? Lay::values(n) : 0) + place.z * Lay::kRow + sub * 8 * Lay::kBytes);
       top_at[i] = page + (head + (value ? Lay::value_max(n) : Lay::key_max(n)) + place.z * 2);
@@ -282,8 +281,8 @@ static int launch_rows(const et_kv_cache &cache, const et_kv_seqs &seqs, const i
   const int per_block = rows_per_block(rows, cache);
   return kv_dispatch(cache.head_dim, cache.format, [&](auto hd, auto fmt) {
     kv_rows_kernel<hd.value, fmt.value, STORE><<<(rows + per_block - 1) / per_block, 256, 0, stream>>>(
-        cu, seqs.kv_len_dev, seqs.page_table_dev, seqs.n_seqs, rows, per_block, seqs.table_stride, seqs.pages_per_seq, c.n_pages, c.page_shift,
-        c.kv_heads, c.data, c.page_bytes, k, k_stride, v, v_stride);
+        cu, seqs.kv_len_dev, seqs.page_table_dev, seqs.n_seqs, rows, per_block, seqs.table_stride, seqs.pages_per_seq, c.page_shift, c,
+        k, k_stride, v, v_stride);
     ET_LAUNCH_CHECK();
     return ET_OK;
   });

@@ -200,12 +200,21 @@ struct Values {
 // A workgroup takes one part of a sequence's tokens for up to 16 query heads of one key-value head; its wavefronts take tiles of
 // 32 tokens in turn.  The cache's bytes go to registers in MFMA operand order, no LDS on the way.
 // The kernel is bound by reading the cache, once.
+struct PagedMore {                                       // the kernel's arguments that its first loads do not need
+  const uint16_t *q;
+  int64_t q_stride;
+  char *data;
+  int64_t page_bytes;
+  float *part_o;
+  float2 *part_ml;
+  uint16_t *out;
+  int n_pages;
+  float scale_log2;
+};
 template <int HD, int FMT>
 __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 2 : 3) void paged_attention_kernel(const int32_t *len, const int32_t *table, int n_seqs,
                                                                       int share, int bound, int window, int units, int row_tiles,
-                                                                      int page_shift, int table_stride, const uint16_t *q, int64_t q_stride,
-                                                                      char *data, int64_t page_bytes, int n_pages, int group, float scale_log2,
-                                                                      float *part_o, float2 *part_ml, uint16_t *out) {
+                                                                      int page_shift, int table_stride, int group, PagedMore o) {
   using Lay = KvLayout<HD, FMT>;
   using K = Keys<HD, FMT>;
   using V = Values<HD, FMT>;
@@ -241,10 +250,10 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 2 : 3) void paged_attention
   auto fetch_pages = [&](int t) {
     const int pos = start + (t + (lane >> 1) * kWaves) * kTile + (lane & 1) * 16;
     page_of = pos < end ? row[pos >> page_shift] : -1;
-    if (page_of >= n_pages) page_of = -1;
+    if (page_of >= o.n_pages) page_of = -1;
   };
   // (A group without a page reads the first page's bytes, and its tokens do not count.)
-  auto head_of = [&](int page) { return data + max(page, 0) * page_bytes + (int64_t)kv * Lay::head_bytes(ps); };
+  auto head_of = [&](int page) { return o.data + max(page, 0) * o.page_bytes + (int64_t)kv * Lay::head_bytes(ps); };
   struct Tile {
     uint32_t kw[2][K::NREG];
     uint2 km[2], vm[2];
@@ -271,7 +280,7 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 2 : 3) void paged_attention
     const int d = K::dim(st, g);
     qf[st] = u32x4{0, 0, 0, 0};
     if (r < live && d < HD)
-      qf[st] = *reinterpret_cast<const u32x4 *>(q + b * q_stride + ((int64_t)kv * group + rt * 16 + r) * HD + d);
+      qf[st] = *reinterpret_cast<const u32x4 *>(o.q + b * o.q_stride + ((int64_t)kv * group + rt * 16 + r) * HD + d);
   }
   load_keys(next, wave, 0);
   for (int t = wave, i = 0; t < tiles; t += kWaves) {
@@ -300,7 +309,7 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 2 : 3) void paged_attention
       for (int st = 0; st < K::STEPS; ++st) d = mfma16(K::operand(kw[u], st, g), qf[st], d);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float f = scale_log2;
+        float f = o.scale_log2;
         if constexpr (FMT != ET_KV_BF16) f *= e & 1 ? bf16hi_to_f32(e & 2 ? km[u].y : km[u].x) : bf16lo_to_f32(e & 2 ? km[u].y : km[u].x);
         z[4 * u + e] = whole_product(d[e], f);
       }
@@ -389,27 +398,27 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 2 : 3) void paged_attention
       }
     }
     for (int d = (threadIdx.x >> 4) * 8; h < live && d < BD; d += 4 * kWaves * 8) {
-      float o[8];
+      float x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        o[e] = 0.f;
+        x[e] = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) o[e] = fmaf(f[w], lds_o[w][d + e][h], o[e]);
+        for (int w = 0; w < kWaves; ++w) x[e] = fmaf(f[w], lds_o[w][d + e][h], x[e]);
       }
       if (part.count == 1) {
         const float inv = total == 0.f ? 0.f : value_factor<FMT>() / total;
         u32x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = cvt_pk_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
-        *reinterpret_cast<u32x4 *>(out + head * HD + blk * BD + d) = v;
+        for (int e = 0; e < 4; ++e) v[e] = cvt_pk_bf16(x[2 * e] * inv, x[2 * e + 1] * inv);
+        *reinterpret_cast<u32x4 *>(o.out + head * HD + blk * BD + d) = v;
       } else {
-        float *to = part_o + slot * HD + blk * BD + d;
-        *reinterpret_cast<f32x4 *>(to) = f32x4{o[0], o[1], o[2], o[3]};
-        *reinterpret_cast<f32x4 *>(to + 4) = f32x4{o[4], o[5], o[6], o[7]};
+        float *to = o.part_o + slot * HD + blk * BD + d;
+        *reinterpret_cast<f32x4 *>(to) = f32x4{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<f32x4 *>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
       }
     }
   }
-  if (part.count > 1 && threadIdx.x < live) part_ml[slot] = make_float2(top, total);
+  if (part.count > 1 && threadIdx.x < live) o.part_ml[slot] = make_float2(top, total);
 }
 
 // Joins the parts of one query head, always in the same order: groups of lanes, four dimensions a lane, take every GROUPS-th part,
@@ -549,7 +558,7 @@ int et_attention_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, const u
   return kv_dispatch(cache->head_dim, cache->format, [&](auto hd, auto fmt) {
     paged_attention_kernel<hd.value, fmt.value><<<(unsigned)(p.items * p.units), 64 * kWaves, 0, stream>>>(
         seqs->kv_len_dev, seqs->page_table_dev, seqs->n_seqs, p.share, p.bound, window, p.units, p.row_tiles, c.page_shift, seqs->table_stride,
-        q_dev, q_stride, c.data, c.page_bytes, c.n_pages, p.group, scale_log2, part_o, part_ml, out_dev);
+        p.group, PagedMore{q_dev, q_stride, c.data, c.page_bytes, part_o, part_ml, out_dev, c.n_pages, scale_log2});
     ET_LAUNCH_CHECK();
     if (p.share) {
       const bool few = p.share <= 16 * (int64_t)seqs->n_seqs;
