@@ -650,9 +650,10 @@ class KVCache:
         elif _dev(out, torch.bfloat16, "out").numel() != n * width or out.device != self.device:
             raise ValueError("out must hold [%d, %d] values on %s" % (n, width, self.device))
         need = lib.et_attention_paged_workspace_bytes(self._cache, seqs, heads, max_len, window)
-        ws = torch.empty((need,), dtype=torch.uint8, device=self.device).data_ptr() if need else None
+        ws = torch.empty((need,), dtype=torch.uint8, device=self.device) if need else None
         _check(lib.et_attention_paged(self._cache, seqs, q.data_ptr(), self._stride(q), heads, max_len, window,
-                                      self._scale if scale is None else float(scale), ws, need, out.data_ptr(), s))
+                                      self._scale if scale is None else float(scale), ws.data_ptr() if need else None, need,
+                                      out.data_ptr(), s))
         return out
 
     def _rows(self, t, name, width):

@@ -104,8 +104,7 @@ __device__ __forceinline__ float value_factor() { return FMT == ET_KV_BF16 ? 1.f
 template <int FMT, int SEL>
 __device__ __forceinline__ uint32_t code_pair(uint32_t w) {
   if constexpr (FMT == ET_KV_E4M3) {
-    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-    const bf16x2_t v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, SEL != 0);
+    const bf16x2 v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, SEL != 0);
     return __builtin_bit_cast(uint32_t, v);
   } else {
     const float a = (float)(int8_t)(w >> (16 * SEL)), b = (float)(int8_t)(w >> (16 * SEL + 8));
@@ -125,7 +124,6 @@ struct Keys {
     return WIDE || s >= 2 * PAIRS ? s * 32 + g * 8 : (s / 2) * 64 + g * 16 + (s % 2) * 8;
   }
   // Past the row's end the last dimensions are read again (and not used).
-  static __device__ __forceinline__ uint32_t lane_off(int r, int g) { return r * kRow + g * 16; }
   static __device__ __forceinline__ void load(const char *base, int r, int g, uint32_t (&w)[NREG]) {
     if constexpr (WIDE) {
 #pragma unroll

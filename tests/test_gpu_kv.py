@@ -390,6 +390,52 @@ def test_attention_reads_strided_queries_and_tables_and_repeats_its_bits():
     assert np.abs(longer - a).max() <= 2.0 ** -6 * np.abs(a).max()    # another split: other roundings only
 
 
+@pytest.mark.parametrize("fmt,page,kv,heads,d,lens,window", [
+    ("int8", 16, 2, 8, 64, [0, 1, 700, 33, 129, 16, 0, 511] * 19, 0),             # 152 sequences: their lengths are scanned in three steps
+    ("bf16", 32, 1, 5, 80, list(range(0, 130)), 0),
+    ("e4m3", 16, 1, 4, 96, [1000, 0, 3, 640, 1500] * 14, 600),
+    ("bf16", 64, 16, 32, 64, [9000, 1, 7000, 0, 12000, 300, 9500], 0),             # long parts, and shorter ones in their place
+    ("e4m3", 256, 32, 32, 128, [5000, 4097, 128, 6000], 0),
+    ("int8", 128, 8, 24, 256, [20000], 0),                                          # a single sequence in many parts
+    ("bf16", 16, 8, 8, 128, [513], 0),
+    ("bf16", 16, 8, 8, 128, [40000, 513, 2], 520),
+])
+def test_attention_of_many_and_of_long_sequences(fmt, page, kv, heads, d, lens, window):
+    """Against float64 on what the cache reads back, with the bound of check_attention."""
+    rng = np.random.default_rng(17)
+    g = torch.Generator("cuda:0").manual_seed(17)
+    table, n_pages = tables(rng, lens, page)
+    cache = et.KVCache(n_pages, page, kv, d, fmt=fmt)
+    cache.data.fill_(0xFF)
+    rows = sum(lens)
+    x = torch.randn((rows, 2 * kv * d), generator=g, device="cuda:0").to(torch.bfloat16)
+    q = torch.randn((len(lens), heads * d), generator=g, device="cuda:0").to(torch.bfloat16)
+    args = dev(table), dev(np.array(lens, dtype=np.int32))
+    cu = dev(np.concatenate([[0], np.cumsum(lens)]).astype(np.int32))
+    cache.append(x[:, :kv * d], x[:, kv * d:], *args, cu)
+    # float64 values of what is held: the codes are those of the rows (tested above)
+    held = x.double().reshape(rows, 2, kv, d)
+    if fmt != "bf16":
+        m = held.abs().amax(-1, keepdim=True)
+        y = held * O.QMAX[fmt] / m
+        held = (torch.round(y) if fmt == "int8" else y.float().to(torch.float8_e4m3fn).double()) * m / O.QMAX[fmt]
+    got = cache.attend(q, *args, max(lens), window=window).double().reshape(len(lens), kv, heads // kv, d)
+    at = 0
+    for b, n in enumerate(lens):
+        lo = at + (max(0, n - window) if window else 0)
+        k, v = (held[lo:at + n, j].transpose(0, 1).contiguous() for j in range(2))            # [kv, tokens, d]
+        qb = q[b].double().reshape(kv, heads // kv, d)
+        if n == 0:
+            assert not got[b].any()
+            continue
+        w = torch.softmax(qb @ k.transpose(1, 2).contiguous() / math.sqrt(d), -1)
+        size = (qb.abs() @ k.abs().transpose(1, 2).contiguous()).amax(-1, keepdim=True) / math.sqrt(d)
+        ref, mass = w @ v, w @ v.abs()
+        tol = 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2 * (d + 8) * 2.0 ** -24 * 1.45 * size + 2 * n * 2.0 ** -24 + 2.0 ** -21) * mass
+        assert ((got[b] - ref).abs() <= tol).all(), (b, n, float(((got[b] - ref).abs() - tol).max()))
+        at += n
+
+
 def test_pages_past_four_gigabytes():
     """Pages whose byte offset needs more than 32 bits: stored, read back and attended to."""
     rng = np.random.default_rng(16)
