@@ -48,11 +48,13 @@ struct Part {
   int len;                                               // of the sequence
   uint32_t per, before;                                  // blocks of a part; parts of the sequences before this one
 };
-// Part number `item`, or (of_seq >= 0) what belongs to that sequence.  The same in all lanes.
+// Part number `item`, or (of_seq >= 0) what belongs to that sequence.  The same in all lanes.  ONE: there is one sequence; without the
+// scans' code beside it each kernel of such a call is 0.2 us shorter.
+template <bool ONE>
 __device__ __forceinline__ Part find_part(const PagedArgs &a, int item, int of_seq) {
   const int lane = threadIdx.x & 63;
   Part p{-1, 0, 0, 0, 1, 0};
-  if (a.n_seqs == 1) {                                   // (shorter than the scans, and one user waits for the answer)
+  if constexpr (ONE) {
     p.len = a.len[0];
     const uint32_t blocks = SeqRange(p.len, a.bound, a.window).blocks();
     p.per = part_blocks(a, blocks);
@@ -61,21 +63,22 @@ __device__ __forceinline__ Part find_part(const PagedArgs &a, int item, int of_s
     if (of_seq >= 0 || item < p.count) p.seq = 0;
     return p;
   }
-  int len = 0, total = 0;
-  uint32_t mine = 0;
-  for (int i = lane; i < a.n_seqs; i += 64) {
-    len = a.len[i];
-    mine = SeqRange(len, a.bound, a.window).blocks();
-    total += mine;
+  auto len_of = [&](int i) { return i < a.n_seqs ? a.len[i] : 0; };
+  int len = len_of(lane), ahead = 0, total = (int)SeqRange(len, a.bound, a.window).blocks();
+  if (a.n_seqs > 64) ahead = len_of(lane + 64);
+  for (int i = lane + 64; i - lane < a.n_seqs; i += 256) {  // (four loads in flight)
+    int l[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) l[u] = len_of(i + 64 * u);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) total += (int)SeqRange(l[u], a.bound, a.window).blocks();
   }
   total = __builtin_amdgcn_readlane(wave_inclusive_scan(total), 63);
   p.per = part_blocks(a, total);
   for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
-    if (a.n_seqs > 64) {
-      len = i0 + lane < a.n_seqs ? a.len[i0 + lane] : 0;
-      mine = SeqRange(len, a.bound, a.window).blocks();
-    }
-    const int parts = (mine + p.per - 1) / p.per, upto = wave_inclusive_scan(parts);
+    int after = 0;
+    if (i0 + 128 < a.n_seqs) after = len_of(i0 + 128 + lane);
+    const int parts = (SeqRange(len, a.bound, a.window).blocks() + p.per - 1) / p.per, upto = wave_inclusive_scan(parts);
     const uint64_t found = of_seq < 0 ? __ballot((uint32_t)item < p.before + upto) : of_seq < i0 + 64 ? 1ull << (of_seq & 63) : 0;
     if (found) {
       const int at = __builtin_ctzll(found);
@@ -87,6 +90,8 @@ __device__ __forceinline__ Part find_part(const PagedArgs &a, int item, int of_s
       return p;
     }
     p.before += __builtin_amdgcn_readlane(upto, 63);
+    len = ahead;
+    ahead = after;
   }
   return p;
 }
@@ -209,7 +214,7 @@ struct PagedMore {                                       // the kernel's argumen
   int n_pages;
   float scale_log2;
 };
-template <int HD, int FMT>
+template <int HD, int FMT, bool ONE>
 __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 2 : 3) void paged_attention_kernel(const int32_t *len, const int32_t *table, int n_seqs,
                                                                       int share, int bound, int window, int units, int row_tiles,
                                                                       int page_shift, int table_stride, int group, PagedMore o) {
@@ -227,7 +232,7 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 2 : 3) void paged_attention
   const int live = min(16, group - rt * 16);              // query heads of this workgroup
   Part part{item, 0, 1, 0, 0, 0};
   if (a.share) {
-    part = find_part(a, item, -1);
+    part = find_part<ONE>(a, item, -1);
     if (part.seq < 0) return;
   } else {
     part.len = a.len[item];
@@ -422,7 +427,7 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 2 : 3) void paged_attention
 // Joins the parts of one query head, always in the same order: groups of lanes, four dimensions a lane, take every GROUPS-th part,
 // and their sums are added up in the groups' order; the loads of eight parts of a group are in flight together.  A head whose
 // sequence is one part has its result already.  THREADS: 64 where a sequence has few parts.
-template <int HD, int FMT, int THREADS>
+template <int HD, int FMT, int THREADS, bool ONE>
 __global__ __launch_bounds__(THREADS) void paged_join_kernel(const int32_t *len, const float *part_o, const float2 *part_ml, int n_seqs,
                                                              int share, int bound, int window, int n_heads, uint16_t *out) {
   constexpr int LANES = HD / 4, GROUPS = THREADS / LANES, BATCH = 8, WAVES = THREADS / 64;
@@ -433,18 +438,21 @@ __global__ __launch_bounds__(THREADS) void paged_join_kernel(const int32_t *len,
   f32x4 v[BATCH];
   float2 s[BATCH];
   auto load = [&](int before, int first, int last) {
+    const int64_t base = (int64_t)before * n_heads + h;
+    const float2 *my_ml = part_ml + base;
+    const float *my_o = part_o + base * HD;
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) {
-      const int64_t at = (int64_t)(before + min(first + i * GROUPS, last)) * n_heads + h;
-      s[i] = part_ml[at];
-      v[i] = reinterpret_cast<const f32x4 *>(part_o + at * HD)[lane];
+      const uint32_t at = (uint32_t)min(first + i * GROUPS, last) * n_heads;
+      s[i] = my_ml[at];
+      v[i] = *reinterpret_cast<const f32x4 *>(my_o + (at * HD + lane * 4));
     }
   };
   // a single sequence's parts come first, however many there are: their loads need not wait for its length
-  if (n_seqs == 1 && grp < GROUPS) load(0, grp, share - 1);
-  const Part p = find_part(a, 0, b);
+  if (ONE && grp < GROUPS) load(0, grp, share - 1);
+  const Part p = find_part<ONE>(a, 0, b);
   if (p.count == 1) return;
-  if (n_seqs > 1 && grp < GROUPS && p.count) load(p.before, grp, p.count - 1);
+  if (!ONE && grp < GROUPS && p.count) load(p.before, grp, p.count - 1);
   const float2 *ml = part_ml + (int64_t)p.before * n_heads + h;
   float top = -INFINITY;
   for (int i = tid; i < p.count; i += THREADS) top = fmaxf(top, ml[(int64_t)i * n_heads].x);
@@ -497,7 +505,12 @@ static PagedPlan paged_plan(const et_kv_cache &c, const et_kv_seqs &s, int n_hea
   p.bound = std::min(max_len, s.pages_per_seq * c.page_size);
   const int span = window > 0 ? (int)std::min<int64_t>(p.bound, (int64_t)window + 15) : p.bound;
   const int64_t blocks = (int64_t)s.n_seqs * ((span + kBlock - 1) / kBlock);
-  p.share = span <= 4 * kBlock ? 0 : (int)std::min<int64_t>(blocks, (kShare + p.units - 1) / p.units);
+  // One part each where that is as fast: short sequences, and longer ones that fill the chip by themselves.  us as one part / shared out:
+  // 1 x 197 tokens 4.7 / 6.7, 256 x 500 of 4 key-value heads 52 / 63, 4 x 1000 of 32 14.5 / 17.0, 1024 x 100 to 2048 of 4 220 / 275; but
+  // 1 x 700 of 8 10.2 / 7.8, 4 x 1500 of 4 16.1 / 9.2, 64 x 1000 to 16384 of 8 256 / 214.
+  const int64_t all = (int64_t)s.n_seqs * p.units;
+  const bool whole = span <= 512 || (span <= 1024 && all >= 64) || (span <= 2048 && all >= 1024);
+  p.share = whole ? 0 : (int)std::min<int64_t>(blocks, (kShare + p.units - 1) / p.units);
   p.items = p.share * (s.n_seqs > 1 ? kFiner : 1) + (int64_t)s.n_seqs;
   p.slots = p.share ? (size_t)p.items * n_heads : 0;
   p.bytes = p.slots * (c.head_dim * sizeof(float) + sizeof(float2));
@@ -554,15 +567,18 @@ int et_attention_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, const u
   const float scale_log2 = scale * 1.4426950408889634f * (cache->format == ET_KV_BF16 ? 1.f : cache->format == ET_KV_INT8 ? 1.f / 127.f : 1.f / 448.f);
   const KvPages c = kv_pages(*cache);
   return kv_dispatch(cache->head_dim, cache->format, [&](auto hd, auto fmt) {
-    paged_attention_kernel<hd.value, fmt.value><<<(unsigned)(p.items * p.units), 64 * kWaves, 0, stream>>>(
+    const bool one = seqs->n_seqs == 1;
+    (one ? paged_attention_kernel<hd.value, fmt.value, true> : paged_attention_kernel<hd.value, fmt.value, false>)<<<
+        (unsigned)(p.items * p.units), 64 * kWaves, 0, stream>>>(
         seqs->kv_len_dev, seqs->page_table_dev, seqs->n_seqs, p.share, p.bound, window, p.units, p.row_tiles, c.page_shift, seqs->table_stride,
         p.group, PagedMore{q_dev, q_stride, c.data, c.page_bytes, part_o, part_ml, out_dev, c.n_pages, scale_log2});
     ET_LAUNCH_CHECK();
     if (p.share) {
-      const bool few = p.share <= 16 * (int64_t)seqs->n_seqs;
+      const bool few = !one && p.share <= 16 * (int64_t)seqs->n_seqs;
       const unsigned heads = (unsigned)(seqs->n_seqs * n_heads);
-      (few ? paged_join_kernel<hd.value, fmt.value, 64> : paged_join_kernel<hd.value, fmt.value, 256>)<<<heads, few ? 64 : 256, 0, stream>>>(
-          seqs->kv_len_dev, part_o, part_ml, seqs->n_seqs, p.share, p.bound, window, n_heads, out_dev);
+      (one ? paged_join_kernel<hd.value, fmt.value, 256, true> : few ? paged_join_kernel<hd.value, fmt.value, 64, false>
+                                                                     : paged_join_kernel<hd.value, fmt.value, 256, false>)<<<
+          heads, few ? 64 : 256, 0, stream>>>(seqs->kv_len_dev, part_o, part_ml, seqs->n_seqs, p.share, p.bound, window, n_heads, out_dev);
       ET_LAUNCH_CHECK();
     }
     return ET_OK;
