@@ -227,8 +227,16 @@ __global__ __launch_bounds__(64 * kWaves, HD > 128 ? 2 : 3) void paged_attention
   __shared__ float2 lds_ml[kWaves][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
   const PagedArgs a{len, n_seqs, bound, window, share};
-  const int item = blockIdx.x / units, unit = blockIdx.x % units, rt = unit % row_tiles, kv = unit / row_tiles;
-  const int n_heads = group * (units / row_tiles), ps = 1 << page_shift;
+  // The row tiles of one part and key-value head are eight workgroups apart: on the same XCD, whose L2 gives them the bytes twice.
+  const int kv_heads = units / row_tiles;
+  int place = blockIdx.x, rt = 0;
+  if (row_tiles > 1) {
+    const int turn = 8 * row_tiles, first = place / turn * 8, width = min(8, (int)gridDim.x / row_tiles - first);
+    rt = place % turn / width;
+    place = first + place % turn % width;
+  }
+  const int item = place / kv_heads, kv = place % kv_heads;
+  const int n_heads = group * kv_heads, ps = 1 << page_shift;
   const int live = min(16, group - rt * 16);              // query heads of this workgroup
   Part part{item, 0, 1, 0, 0, 0};
   if (a.share) {
