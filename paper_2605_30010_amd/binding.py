@@ -662,7 +662,8 @@ class KVCache:
             raise TypeError("%s must be a bfloat16 tensor on %s" % (name, self.device))
         if t.dim() == 3 and t.shape[2] == self.head_dim and (t.stride(1) == self.head_dim or t.shape[1] == 1):
             t = t.as_strided((t.shape[0], t.shape[1] * t.shape[2]), (t.stride(0), t.stride(2)))
-        if t.dim() != 2 or t.stride(1) != 1 or t.shape[1] % self.head_dim or (width and t.shape[1] != width):
+        shape = t.shape
+        if len(shape) != 2 or t.stride(1) != 1 or (shape[1] != width if width else shape[1] % self.head_dim):
             heads = width // self.head_dim or "n_heads"
             raise ValueError("%s must be [rows, %s * head_dim] or [rows, %s, head_dim] with contiguous rows" % (name, heads, heads))
         return t
@@ -672,23 +673,24 @@ class KVCache:
         n, width = t.shape
         return t.stride(0) if n > 1 else width                        # (the stride of a single row says nothing)
 
+    def _ints(self, t, name):
+        if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.device == self.device):
+            raise TypeError("%s must be an int32 tensor on %s" % (name, self.device))
+        return t.shape
+
     def _seqs(self, page_table, kv_len):
-        for t, name in ((page_table, "page_table"), (kv_len, "kv_len")):
-            if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.device == self.device):
-                raise TypeError("%s must be an int32 tensor on %s" % (name, self.device))
-        if page_table.dim() != 2 or page_table.shape[1] < 1 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        shape = self._ints(page_table, "page_table")
+        if len(shape) != 2 or shape[1] < 1 or (shape[1] > 1 and page_table.stride(1) != 1):
             raise ValueError("page_table must be [n_seqs, pages] with contiguous rows")
-        n, pages = page_table.shape
-        if kv_len.dim() != 1 or kv_len.shape[0] != n or not kv_len.is_contiguous():
+        n, pages = shape
+        if self._ints(kv_len, "kv_len") != (n,) or not kv_len.is_contiguous():
             raise ValueError("kv_len must be contiguous, one for each row of page_table")
         return _KvSeqs(page_table.data_ptr(), page_table.stride(0) if n > 1 else pages, pages, kv_len.data_ptr(), n)
 
     def _cu(self, cu_rows, kv_len):
         if cu_rows is None:
             return None
-        if not (isinstance(cu_rows, torch.Tensor) and cu_rows.dtype is torch.int32 and cu_rows.device == self.device):
-            raise TypeError("cu_rows must be an int32 tensor on %s" % self.device)
-        if cu_rows.dim() != 1 or cu_rows.shape[0] != kv_len.shape[0] + 1 or not cu_rows.is_contiguous():
+        if self._ints(cu_rows, "cu_rows") != (kv_len.shape[0] + 1,) or not cu_rows.is_contiguous():
             raise ValueError("cu_rows must be contiguous, one more than there are sequences")
         return cu_rows.data_ptr()
 
