@@ -82,9 +82,9 @@ __device__ __forceinline__ uint32_t group_max(uint32_t v) {
 }
 
 // The codes of eight values (bf16 pairs) of a row whose largest magnitude has the bits `top`.  code = round(x Q / m): both
-// are taken times a power of two that brings m into [1/2, 1), so nothing overflows; x Q is exact (8 + 7 bits), and the
-// corrected product is the correctly rounded quotient: one of two 8-bit numbers and Q lies on a tie or at least 2^-9 of a
-// step from it, so every code is the one of exact arithmetic.
+// are taken times a power of two that brings m into [1/2, 1), so nothing overflows; x Q is exact (8 + 9 bits), and the
+// corrected product is the correctly rounded quotient.  A quotient of two 8-bit numbers times Q lies on a tie of the codes or at least 2^-13 of
+// a step from it (the smallest e4m3 steps; 2^-9 elsewhere), so every code is the one of exact arithmetic.
 template <int FMT>
 __device__ __forceinline__ uint2 quantise8(u32x4 x, uint32_t top) {
   const float m = __uint_as_float(top << 16);

@@ -367,6 +367,25 @@ def test_attention_of_infinities_and_nan():
         assert (np.abs(got[0, h] - ref[0]) <= 2.0 ** -8 * np.abs(ref[0]) + (2.0 ** -8 + 1e-4) * mass[0]).all()
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("window", [1, 7, 16, 40])
+def test_attention_does_not_see_what_is_masked(fmt, window):
+    """Rows of NaN and infinities in front of the window, in the window's first group of 16 too, change nothing."""
+    rng = np.random.default_rng(18)
+    lens, page = [50, 33, 200, 17], 16
+    table, n_pages = tables(rng, lens, page)
+    host = Pages(n_pages, page, 2, 80, fmt, fill=0xFF)
+    tokens = fill(host, table, lens, rng)
+    for b, n in enumerate(lens):
+        for pos in range(max(0, n - window)):
+            row = np.full((2, 80), [np.nan, np.inf, -np.inf][pos % 3])
+            for value in (False, True):
+                host.put(*O.place(pos, table[b], n_pages, page), row, value)
+    q = bf16(rng.normal(size=(len(lens), 6, 80)))
+    got = check_attention(host, table, lens, tokens, q, 6, window=window)
+    assert np.isfinite(got).all() and got.any()
+
+
 def test_attention_reads_strided_queries_and_tables_and_repeats_its_bits():
     rng = np.random.default_rng(15)
     lens, page, heads, d = [3000, 77, 1500], 32, 14, 128
@@ -399,6 +418,8 @@ def test_attention_reads_strided_queries_and_tables_and_repeats_its_bits():
     ("int8", 128, 8, 24, 256, [20000], 0),                                          # a single sequence in many parts
     ("bf16", 16, 8, 8, 128, [513], 0),
     ("bf16", 16, 8, 8, 128, [40000, 513, 2], 520),
+    ("int8", 16, 64, 64, 64, [45000], 0),                                          # parts of more than 64 groups of 16 tokens a wavefront
+    ("e4m3", 64, 64, 64, 80, [61000, 61003, 4], 0),
 ])
 def test_attention_of_many_and_of_long_sequences(fmt, page, kv, heads, d, lens, window):
     """Against float64 on what the cache reads back, with the bound of check_attention."""
