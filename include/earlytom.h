@@ -394,10 +394,14 @@ int et_kv_read(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *
  * t running over the last `window` positions below kv_len[b] (window = 0: all of them) that have a page.  A head
  * that no token is left for, or whose logits are all minus infinity, gets zeros.  q_dev bf16 [n_seqs, n_heads *
  * head_dim] with row stride q_stride (a multiple of 8; aligned to 16 bytes); out_dev bf16 [n_seqs, n_heads * head_dim],
- * contiguous, not q_dev.  max_len: a bound of every kv_len that the host knows (positions from max_len on are left out); it decides how the
- * work is split, a generous one costs little.  Two equal calls give equal bits.  workspace: et_attention_paged_workspace_bytes
- * with the same arguments, contents arbitrary; calls that run at the same time need one each.  Asynchronous on `hip_stream`.
- * Errors: INVALID_ARG, UNSUPPORTED (page_size, head_dim), WORKSPACE, HIP. */
+ * contiguous, not q_dev.  max_len: a bound of every kv_len that the host knows (positions from max_len on are left out).  The tokens
+ * of all sequences are shared out evenly over the chip's workgroups on the device, by the lengths it finds there, so a generous bound
+ * costs little; sequences that are short by their bound are one part each.  Two equal calls give equal bits; a sequence beside
+ * others, or under another bound, may be split elsewhere, which moves its result within the rounding.  Logits, their maximum, the
+ * sums and the products' accumulators are float32, the weights bfloat16.  workspace: et_attention_paged_workspace_bytes with the same
+ * arguments, contents arbitrary, aligned to 16 bytes; calls that run at the same time need one each.  n_seqs * n_heads at most 2^24,
+ * n_seqs * max_len at most 2^36.  Asynchronous on `hip_stream`.  Errors: INVALID_ARG, UNSUPPORTED (page_size, head_dim),
+ * WORKSPACE, HIP. */
 size_t et_attention_paged_workspace_bytes(const et_kv_cache *cache, const et_kv_seqs *seqs, int32_t n_heads,
                                           int32_t max_len, int32_t window);
 int et_attention_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, const uint16_t *q_dev, int64_t q_stride,

@@ -579,8 +579,9 @@ class KVCache:
     """A paged key-value cache: `data` uint8 [n_pages, page bytes] on the device (layout in earlytom.h), allocated here unless
     given.  fmt: "bf16", "e4m3" or "int8".  The sequences are the caller's: page_table int32 [n_seqs, pages] (entries outside
     [0, n_pages) = no page; rows may be strided), kv_len int32 [n_seqs].  Every call is asynchronous on `stream` (default: the
-    current stream of the cache's device), allocates with torch's allocator only, keeps nothing, and can be captured into a
-    graph; calls on several streams may run at the same time as long as none of them stores what another one reads."""
+    current stream of the cache's device; results and workspaces are allocated there, so a result belongs to that stream),
+    keeps nothing, and can be captured into a graph; calls on several streams may run at the same time as long as none of
+    them stores what another one reads."""
 
     def __init__(self, n_pages, page_size, n_kv_heads, head_dim, fmt="bf16", data=None, device="cuda:0"):
         if fmt not in _KV_FORMATS:
@@ -623,7 +624,8 @@ class KVCache:
         seqs, cu = self._seqs(page_table, kv_len), self._cu(cu_rows, kv_len)
         rows = kv_len.shape[0] if rows is None else int(rows)
         if out is None:
-            k, v = (torch.empty((max(rows, 0), self._width), dtype=torch.bfloat16, device=self.device) for _ in range(2))
+            k = torch.empty((max(rows, 0), self._width), dtype=torch.bfloat16, device=self.device)
+            v = torch.empty_like(k)
             out = k, v
         else:
             k, v = self._rows(out[0], "out[0]", self._width), self._rows(out[1], "out[1]", self._width)
@@ -646,7 +648,7 @@ class KVCache:
             raise ValueError("q has %d rows for %d sequences" % (n, kv_len.shape[0]))
         heads, max_len, window = width // self.head_dim, int(max_len), int(window)
         if out is None:
-            out = torch.empty((n, width), dtype=torch.bfloat16, device=self.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif _dev(out, torch.bfloat16, "out").numel() != n * width or out.device != self.device:
             raise ValueError("out must hold [%d, %d] values on %s" % (n, width, self.device))
         need = lib.et_attention_paged_workspace_bytes(self._cache, seqs, heads, max_len, window)

@@ -219,10 +219,11 @@ struct PagedMore {                                       // the kernel's argumen
 // logits, reference, sums and accumulators are float32.
 // Bound by the memory side from some 10 MB on: 537 MB of bfloat16 (one sequence of 131072 tokens, 8 key-value heads of 128) in 94 us,
 // 5.7 TB/s, 1.16 GB of e4m3 (64 sequences) in 211, 5.5 TB/s, by the counters 1.00 of these bytes; below that by the chain launch - length - page -
-// keys - products - joined wavefronts, 4.1 us at the least.  Three workgroups per compute unit (two for heads of 256): 168 registers
-// of a lane; left to itself the compiler took 222 and two, 237 instead of 222 us on those 64.
+// keys - products - joined wavefronts, 4.1 us at the least.  Two workgroups per compute unit are asked for: without that the compiler moves
+// the accumulators to and fro between the two halves of the registers, and 32 int8 sequences of up to 5309 tokens take 23.4 instead of
+// 21.6 us, 12 of 2000 to 8000 with 16 heads of 256 119 instead of 100.
 template <int HD, int FMT, bool ONE>
-__global__ __launch_bounds__(64 * kWaves, HD > 128 ? 2 : 3) void paged_attention_kernel(const int32_t *len, const int32_t *table, int n_seqs,
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const int32_t *len, const int32_t *table, int n_seqs,
                                                                       int share, int bound, int window, int units, int row_tiles,
                                                                       int page_shift, int table_stride, int group, PagedMore o) {
   using Lay = KvLayout<HD, FMT>;
