@@ -217,11 +217,11 @@ struct PagedMore {                                       // the kernel's argumen
 // values are loaded to match).  The cache's bytes go to registers in operand order, with no LDS on the way, the next tile's keys while a
 // tile is worked on; nothing is read twice.  Weights are rounded to bfloat16 (half a step, 2^-8 of each; the values' precision is no better),
 // logits, reference, sums and accumulators are float32.
-// Bound by the memory side from some 10 MB on: 537 MB of bfloat16 (one sequence of 131072 tokens, 8 key-value heads of 128) in 94 us,
-// 5.7 TB/s, 1.16 GB of e4m3 (64 sequences) in 211, 5.5 TB/s, by the counters 1.00 of these bytes; below that by the chain launch - length - page -
-// keys - products - joined wavefronts, 4.1 us at the least.  Two workgroups per compute unit are asked for: without that the compiler moves
-// the accumulators to and fro between the two halves of the registers, and 32 int8 sequences of up to 5309 tokens take 23.4 instead of
-// 21.6 us, 12 of 2000 to 8000 with 16 heads of 256 119 instead of 100.
+// Bound by the memory side from some 10 MB on: 537 MB of bfloat16 (one sequence of 131072 tokens, 8 key-value heads of 128) in 91 us,
+// 5.9 TB/s, 1.16 GB of e4m3 (64 sequences) in 208, 5.6 TB/s, by the counters 1.00 of these bytes; below that by the chain launch -
+// length - page - keys - products - joined wavefronts, 4.0 us at the least.  Two workgroups per compute unit are asked for: without that the compiler
+// moves the accumulators to and fro between the two halves of the registers, and 32 int8 sequences of up to 5309 tokens take 23.4
+// instead of 21.6 us, 12 of 2000 to 8000 with 16 heads of 256 119 instead of 100.
 template <int HD, int FMT, bool ONE>
 __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const int32_t *len, const int32_t *table, int n_seqs,
                                                                       int share, int bound, int window, int units, int row_tiles,
@@ -230,6 +230,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
   using K = Keys<HD, FMT>;
   using V = Values<HD, FMT>;
   constexpr int ACC = V::BLOCKS * V::DPL;
+  constexpr bool kAhead = HD <= 128;                      // a tile's keys are fetched during the one before: heads of 256 have no registers for it
   constexpr int BD = HD / V::BLOCKS;                      // dimensions that the wavefronts add up at a time
   __shared__ float lds_o[kWaves][BD][16];
   __shared__ float2 lds_ml[kWaves][16];
@@ -301,8 +302,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
     if (r < live && d < HD)
       qf[st] = *reinterpret_cast<const u32x4 *>(o.q + b * o.q_stride + ((int64_t)kv * group + rt * 16 + r) * HD + d);
   }
-  load_keys(next, wave, 0);
+  if (wave < tiles) load_keys(next, wave, 0);
   for (int t = wave, i = 0; t < tiles; t += kWaves) {
+    if (!kAhead && t != wave) load_keys(next, t, i);
     const Tile cur = next;
     const int pos0 = start + t * kTile;
     const uint2 *km = cur.km, *vm = cur.vm;
@@ -333,7 +335,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
         z[4 * u + e] = whole_product(d[e], f);
       }
     }
-    load_keys(next, t + kWaves, i);
+    if (kAhead && t + kWaves < tiles) load_keys(next, t + kWaves, i);
     // tokens that do not count: no page, past the end, before the window
     const bool whole = page[0] >= 0 && page[1] >= 0 && pos0 >= sr.first && pos0 + kTile <= end;
     uint32_t dead = 0;
