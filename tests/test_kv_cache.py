@@ -2,6 +2,9 @@
 points (nothing is launched)."""
 import ctypes as C
 import math
+import os
+import re
+import subprocess
 
 import numpy as np
 import pytest
@@ -10,6 +13,7 @@ import torch
 import paper_2605_30010_amd as et
 from oracle import kv_oracle as O
 from paper_2605_30010_amd import binding as B
+from paper_2605_30010_amd.build import CSRC, FLAGS, HIPCC
 
 
 def test_oracle_e4m3_values_are_torchs():
@@ -157,3 +161,14 @@ def test_attention_of_too_much_at_once():
     assert attend_call(s=seqs(n_seqs=1 << 23), heads=4) == -1 and "2^24" in et.et_last_error()
     assert attend_call(s=seqs(n_seqs=1 << 20, pages_per_seq=1 << 20, table_stride=1 << 20), max_len=10 ** 6) == -1
     assert "2^36" in et.et_last_error()
+
+
+def test_attention_kernels_keep_to_their_registers(tmp_path):
+    """Two workgroups of four wavefronts share a compute unit: at most 256 registers a lane, none of them in memory."""
+    run = subprocess.run([HIPCC] + FLAGS + ["--offload-device-only", "-Rpass-analysis=kernel-resource-usage", "-c",
+                                            os.path.join(CSRC, "paged_attention.hip"), "-o", str(tmp_path / "paged.o")],
+                         check=True, capture_output=True, text=True)
+    kernels = re.findall(r"Function Name: \S*?(paged_\w+?_kernel)\S*.*?TotalSGPRs.*? VGPRs: (\d+).*? AGPRs: (\d+).*?ScratchSize \[bytes/lane\]: (\d+)",
+                         run.stderr, re.S)
+    assert len(kernels) == 5 * 3 * (2 + 3)
+    assert all(int(v) + int(a) <= 256 and scratch == "0" for _, v, a, scratch in kernels), kernels
