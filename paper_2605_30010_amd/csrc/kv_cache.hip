@@ -264,13 +264,14 @@ static int check_rows(const et_kv_cache *cache, const et_kv_seqs *seqs, const in
   return ET_OK;
 }
 
-// Rows of a workgroup: enough for a group of lanes to have four turns of copying or sixteen of quantising, as long as a thousand
-// workgroups remain.  Measured, us at 1 / 4 / 8 / 16 / 32 rows: 65 600 bfloat16 rows of 8 heads of 128 stored 116 / 110 / 112 /
-// 118 / 118, e4m3 stored and read back 251 / 190 / 177 / 175 / 178; 130 000 bfloat16 rows of 4 heads of 80 read 179 / 93 / 73 / 72 / 77; 5000
-// int8 rows of 4 heads of 128 stored and read back 17.7 / 12.9 / 15.1 / 19.0 / 26.7.
+// Rows of a workgroup: enough for a group of lanes to have four turns of copying or sixteen of quantising (at most the 64 that a
+// wavefront locates), as long as a thousand workgroups remain.  Measured, us at 1 / 4 / 8 / 16 / 32 rows: 65 600 bfloat16 rows of 8 heads of
+// 128 stored 116 / 110 / 112 / 118 / 118, e4m3 stored and read back 251 / 190 / 177 / 175 / 178; 130 000 bfloat16 rows of 4 heads of 80
+// read 179 / 93 / 73 / 72 / 77; 5000 int8 rows of 4 heads of 128 stored and read back 17.7 / 12.9 / 15.1 / 19.0 / 26.7; at 16 / 32 / 64
+// rows: 928 000 int8 rows of 3 heads of 64 read 293 / 261 / 251, 630 000 of one head of 128 stored and read back 259 / 222 / 220.
 static int rows_per_block(int rows, const et_kv_cache &c) {
   const int lanes = c.head_dim <= 64 ? 8 : c.head_dim <= 128 ? 16 : 32, turns = c.format == ET_KV_BF16 ? 4 : 16;
-  return std::max(1, std::min({16, rows / 1024, turns * (256 / lanes) / (2 * c.n_kv_heads)}));
+  return std::max(1, std::min({64, rows / 1024, turns * (256 / lanes) / (2 * c.n_kv_heads)}));
 }
 
 template <bool STORE>
