@@ -114,8 +114,8 @@ __device__ __forceinline__ uint2 quantise8(u32x4 x, uint32_t top) {
 
 // The values (bf16 pairs) of eight codes, code * m / Q rounded once.  The factor m / Q is taken as the sum of two float32
 // numbers, hi the nearest: what is rounded to bfloat16 is then the quotient rounded to float32, and neither rounding can go astray, since a
-// quotient of code m (16 bits at most) by Q lies on a tie of bfloat16 or at least 2^-17 from it, relatively.  int8 codes times
-// hi alone would do: 127 is prime, so no quotient is on a tie.
+// quotient of code m (16 bits at most) by Q lies on a tie of bfloat16 or at least 2^-17 from it, relatively.  For int8 codes
+// hi alone does: 127 is prime, so no quotient is on a tie.
 struct KvFactor {
   float hi, lo;
 };

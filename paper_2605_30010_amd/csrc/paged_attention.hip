@@ -10,7 +10,9 @@ namespace et {
 constexpr int kTile = 32;                                // tokens that a wavefront takes at a time
 constexpr int kWaves = 4;                                // wavefronts of a workgroup
 constexpr int kBlock = kWaves * kTile;
-constexpr int kShare = 512, kFiner = 4;                  // workgroups that a call is shared out over, and how many times as many at most
+// Workgroups that a call is shared out over: two per compute unit (us at 512 / 768 / 1024: 32 x 0 to 5309 int8 tokens 22.6 / 23.2 / 26.0,
+// 131072 bfloat16 tokens 95 / 96 / 97); and how many times as many at most (see part_blocks).
+constexpr int kShare = 512, kFiner = 4;
 
 // a * b rounded, never part of a fused multiply-add: a logit less the maximum has to be 0 for the maximum itself, however large.
 __device__ __forceinline__ float whole_product(float a, float b) {
@@ -38,7 +40,7 @@ struct SeqRange {
   __device__ __forceinline__ uint32_t blocks() const { return hi > lo ? (uint32_t)(hi - lo + kBlock - 1) / kBlock : 0; }
 };
 // Blocks of a part.  Sequences seldom end with a whole part, so where there are several and the parts are long, shorter ones even
-// out what the last parts leave over.
+// out what the last parts leave over: 64 x 1000 to 16384 e4m3 tokens 241 -> 214 us, 12 x 2000 to 8000 with heads of 256 115 -> 100.
 __device__ __forceinline__ uint32_t part_blocks(const PagedArgs &a, uint32_t total) {
   const uint32_t per = max((total + a.share - 1) / a.share, 1u);
   return a.n_seqs > 1 && per > 8 ? max((per + kFiner - 1) / kFiner, 8u) : per;
@@ -598,6 +600,7 @@ int et_attention_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, const u
         p.group, PagedMore{q_dev, q_stride, c.data, c.page_bytes, part_o, part_ml, out_dev, c.n_pages, scale_log2});
     ET_LAUNCH_CHECK();
     if (p.share) {
+      // (64 / 256 lanes a head, us: 64 x 100 to 2048 tokens, 32 heads 61.6 / 64.9; 2 x 60000, 16 heads, 196 parts each 30.1 / 20.2)
       const bool few = !one && p.share <= 16 * (int64_t)seqs->n_seqs;
       const unsigned heads = (unsigned)(seqs->n_seqs * n_heads);
       (one ? paged_join_kernel<hd.value, fmt.value, 256, true> : few ? paged_join_kernel<hd.value, fmt.value, 64, false>
