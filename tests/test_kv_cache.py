@@ -172,3 +172,67 @@ def test_attention_kernels_keep_to_their_registers(tmp_path):
                          run.stderr, re.S)
     assert len(kernels) == 5 * 3 * (2 + 3)
     assert all(int(v) + int(a) <= 256 and scratch == "0" for _, v, a, scratch in kernels), kernels
+
+
+class _Device:
+    """Stands in for torch.cuda.device and torch.cuda.stream: notes what is current."""
+    current, log = 0, []
+
+    def __init__(self, to):
+        self.to = to
+
+    def __enter__(self):
+        self.was, _Device.current = _Device.current, self.to
+        _Device.log.append(self.to)
+
+    def __exit__(self, *_):
+        _Device.current = self.was
+
+
+class _Lib:
+    """Notes under which device each entry point is called, and with which stream (its last argument)."""
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, _Device.current, args[-1]))
+            return 64 if name.endswith("bytes") else 0
+        return call
+
+
+@pytest.mark.parametrize("current", [0, None])
+def test_calls_run_on_the_caches_device_and_its_stream(monkeypatch, current):
+    """A cache on another device than the current one: allocation and launch happen with its device current, on that device's
+    stream; a stream of a third device is refused.  (Tensors without memory stand for the other device, index None.)"""
+    meta = torch.device("meta")
+    c = object.__new__(et.KVCache)
+    c.device, c.fmt, c.head_dim, c.n_kv_heads, c._width, c._scale, c._cache, c._lib = meta, "bf16", 64, 2, 128, 0.125, None, _Lib()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: _Device.current)
+    monkeypatch.setattr(torch.cuda, "device", lambda d: _Device(d.index))
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: _Device(s.device.index))
+    monkeypatch.setattr(B, "_raw_stream", lambda d: ("stream of", d))
+    _Device.current, _Device.log = current, []
+    x = torch.empty((3, 128), dtype=torch.bfloat16, device=meta)
+    tab, lens = torch.empty((3, 2), dtype=torch.int32, device=meta), torch.empty(3, dtype=torch.int32, device=meta)
+
+    class Stream:
+        device, cuda_stream = meta, 5
+
+    class Other:
+        device, cuda_stream = torch.device("cpu"), 6
+
+    for extra in ({}, {"stream": Stream()}):
+        c._lib.calls.clear()
+        _Device.log.clear()
+        c.append(x, x, tab, lens, **extra)
+        c.read(tab, lens, **extra)
+        c.attend(x, tab, lens, 32, **extra)
+        launches = [k for k in c._lib.calls if not k[0].endswith("bytes")]
+        assert [k[0] for k in launches] == ["et_kv_append", "et_kv_read", "et_attention_paged"]
+        assert all(k[1] is None and k[2] == ("stream of", None) for k in launches)
+        assert _Device.current == current and len(_Device.log) == (3 if extra or current == 0 else 0)
+    for call in (lambda: c.append(x, x, tab, lens, stream=Other()), lambda: c.read(tab, lens, stream=Other()),
+                 lambda: c.attend(x, tab, lens, 32, stream=Other())):
+        with pytest.raises(ValueError):
+            call()
