@@ -565,7 +565,8 @@ class Projector:
             pass
 
 
-# The current stream's handle without an object around it (2 us a call less).
+# The current device, and its current stream's handle without an object around it (2 us a call less).
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 _KV_FORMATS = {"bf16": ET_KV_BF16, "e4m3": ET_KV_E4M3, "int8": ET_KV_INT8}
@@ -607,12 +608,13 @@ class KVCache:
         if s is None:
             with self._elsewhere(stream):
                 return self.append(k, v, page_table, kv_len, cu_rows)
-        k, v = self._rows(k, "k", self._width), self._rows(v, "v", self._width)
-        rows = k.shape[0]
-        if v.shape[0] != rows:
-            raise ValueError("k has %d rows, v %d" % (rows, v.shape[0]))
-        _check(self._lib.et_kv_append(self._cache, self._seqs(page_table, kv_len), self._cu(cu_rows, kv_len), rows, k.data_ptr(),
-                                      self._stride(k), v.data_ptr(), self._stride(v), s))
+        k, rows, _, k_stride = self._rows(k, "k", self._width)
+        v, v_rows, _, v_stride = self._rows(v, "v", self._width)
+        if v_rows != rows:
+            raise ValueError("k has %d rows, v %d" % (rows, v_rows))
+        seqs = self._seqs(page_table, kv_len)
+        _check(self._lib.et_kv_append(self._cache, seqs, None if cu_rows is None else self._cu(cu_rows, kv_len), rows, k.data_ptr(),
+                                      k_stride, v.data_ptr(), v_stride, s))
 
     def read(self, page_table, kv_len, cu_rows=None, rows=None, out=None, stream=None):
         """The last cu_rows[b + 1] - cu_rows[b] tokens of every sequence b (None: one each) as bf16 rows (k, v), [rows,
@@ -621,17 +623,19 @@ class KVCache:
         if s is None:
             with self._elsewhere(stream):
                 return self.read(page_table, kv_len, cu_rows, rows, out)
-        seqs, cu = self._seqs(page_table, kv_len), self._cu(cu_rows, kv_len)
-        rows = kv_len.shape[0] if rows is None else int(rows)
+        seqs = self._seqs(page_table, kv_len)
+        cu = None if cu_rows is None else self._cu(cu_rows, kv_len)
+        rows = seqs.n_seqs if rows is None else int(rows)
         if out is None:
-            k = torch.empty((max(rows, 0), self._width), dtype=torch.bfloat16, device=self.device)
-            v = torch.empty_like(k)
+            k = torch.empty(max(rows, 0), self._width, dtype=torch.bfloat16, device=self.device)
+            v, k_stride, v_stride = torch.empty_like(k), self._width, self._width
             out = k, v
         else:
-            k, v = self._rows(out[0], "out[0]", self._width), self._rows(out[1], "out[1]", self._width)
-            if k.shape[0] < rows or v.shape[0] < rows:
+            k, k_rows, _, k_stride = self._rows(out[0], "out[0]", self._width)
+            v, v_rows, _, v_stride = self._rows(out[1], "out[1]", self._width)
+            if k_rows < rows or v_rows < rows:
                 raise ValueError("out has fewer than %d rows" % rows)
-        _check(self._lib.et_kv_read(self._cache, seqs, cu, rows, k.data_ptr(), self._stride(k), v.data_ptr(), self._stride(v), s))
+        _check(self._lib.et_kv_read(self._cache, seqs, cu, rows, k.data_ptr(), k_stride, v.data_ptr(), v_stride, s))
         return out
 
     def attend(self, q, page_table, kv_len, max_len, window=0, scale=None, out=None, stream=None):
@@ -642,38 +646,36 @@ class KVCache:
         if s is None:
             with self._elsewhere(stream):
                 return self.attend(q, page_table, kv_len, max_len, window, scale, out)
-        q, seqs, lib = self._rows(q, "q", 0), self._seqs(page_table, kv_len), self._lib
-        n, width = q.shape
-        if n != kv_len.shape[0]:
-            raise ValueError("q has %d rows for %d sequences" % (n, kv_len.shape[0]))
+        q, n, width, q_stride = self._rows(q, "q", 0)
+        seqs, lib = self._seqs(page_table, kv_len), self._lib
+        if n != seqs.n_seqs:
+            raise ValueError("q has %d rows for %d sequences" % (n, seqs.n_seqs))
         heads, max_len, window = width // self.head_dim, int(max_len), int(window)
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif _dev(out, torch.bfloat16, "out").numel() != n * width or out.device != self.device:
             raise ValueError("out must hold [%d, %d] values on %s" % (n, width, self.device))
-        need = lib.et_attention_paged_workspace_bytes(self._cache, seqs, heads, max_len, window)
-        ws = torch.empty((need,), dtype=torch.uint8, device=self.device) if need else None
-        _check(lib.et_attention_paged(self._cache, seqs, q.data_ptr(), self._stride(q), heads, max_len, window,
+        # (no workspace up to a bound of 512)
+        need = lib.et_attention_paged_workspace_bytes(self._cache, seqs, heads, max_len, window) if max_len > 512 else 0
+        ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        _check(lib.et_attention_paged(self._cache, seqs, q.data_ptr(), q_stride, heads, max_len, window,
                                       self._scale if scale is None else float(scale), ws.data_ptr() if need else None, need,
                                       out.data_ptr(), s))
         return out
 
     def _rows(self, t, name, width):
-        """t as [rows, columns] with unit column stride (width 0: any number of heads)."""
+        """t as [rows, columns] with unit column stride, and its rows, columns and row stride (width 0: any number of heads)."""
         if not (isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.device == self.device):
             raise TypeError("%s must be a bfloat16 tensor on %s" % (name, self.device))
-        if t.dim() == 3 and t.shape[2] == self.head_dim and (t.stride(1) == self.head_dim or t.shape[1] == 1):
-            t = t.as_strided((t.shape[0], t.shape[1] * t.shape[2]), (t.stride(0), t.stride(2)))
-        shape = t.shape
-        if len(shape) != 2 or t.stride(1) != 1 or (shape[1] != width if width else shape[1] % self.head_dim):
+        shape, strides = t.shape, t.stride()
+        if len(shape) == 3 and shape[2] == self.head_dim and (strides[1] == self.head_dim or shape[1] == 1):
+            shape, strides = (shape[0], shape[1] * shape[2]), (strides[0], strides[2])
+            t = t.as_strided(shape, strides)
+        if len(shape) != 2 or strides[1] != 1 or (shape[1] != width if width else shape[1] % self.head_dim):
             heads = width // self.head_dim or "n_heads"
             raise ValueError("%s must be [rows, %s * head_dim] or [rows, %s, head_dim] with contiguous rows" % (name, heads, heads))
-        return t
-
-    @staticmethod
-    def _stride(t):
-        n, width = t.shape
-        return t.stride(0) if n > 1 else width                        # (the stride of a single row says nothing)
+        n, width = shape
+        return t, n, width, strides[0] if n > 1 else width           # (the stride of a single row says nothing)
 
     def _ints(self, t, name):
         if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.device == self.device):
@@ -681,24 +683,22 @@ class KVCache:
         return t.shape
 
     def _seqs(self, page_table, kv_len):
-        shape = self._ints(page_table, "page_table")
-        if len(shape) != 2 or shape[1] < 1 or (shape[1] > 1 and page_table.stride(1) != 1):
+        shape, strides = self._ints(page_table, "page_table"), page_table.stride()
+        if len(shape) != 2 or shape[1] < 1 or (strides[1] != 1 and shape[1] > 1):
             raise ValueError("page_table must be [n_seqs, pages] with contiguous rows")
         n, pages = shape
         if self._ints(kv_len, "kv_len") != (n,) or not kv_len.is_contiguous():
             raise ValueError("kv_len must be contiguous, one for each row of page_table")
-        return _KvSeqs(page_table.data_ptr(), page_table.stride(0) if n > 1 else pages, pages, kv_len.data_ptr(), n)
+        return _KvSeqs(page_table.data_ptr(), strides[0] if n > 1 else pages, pages, kv_len.data_ptr(), n)
 
     def _cu(self, cu_rows, kv_len):
-        if cu_rows is None:
-            return None
         if self._ints(cu_rows, "cu_rows") != (kv_len.shape[0] + 1,) or not cu_rows.is_contiguous():
             raise ValueError("cu_rows must be contiguous, one more than there are sequences")
         return cu_rows.data_ptr()
 
     def _here(self, stream):
         """The stream to launch on, if its device is the current one and no other stream is asked for."""
-        if stream is None and torch.cuda.current_device() == self.device.index:
+        if stream is None and _current_device() == self.device.index:
             return _raw_stream(self.device.index)
         return None
 

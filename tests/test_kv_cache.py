@@ -147,7 +147,7 @@ def test_attention_workspace():
     lib = et.load_library()
     need = lambda c, s, heads, max_len, window: lib.et_attention_paged_workspace_bytes(C.byref(c), C.byref(s), heads, max_len, window)
     c, long = cache(), seqs(pages_per_seq=1 << 20, table_stride=1 << 20)
-    assert need(c, seqs(), 4, 64, 0) == 0 and need(c, long, 4, 10 ** 6, 64) == 0
+    assert need(c, long, 4, 512, 0) == need(c, seqs(), 4, 64, 0) == 0 and need(c, long, 4, 10 ** 6, 64) == 0
     b = need(c, long, 4, 10 ** 6, 0)
     assert 0 < b <= 64 << 20 and need(c, long, 4, 2 ** 31 - 1, 0) == b
     assert need(c, long, 3, 10 ** 6, 0) == 0 and need(c, long, 4, 0, 0) == 0 and need(cache(head_dim=72), long, 4, 10 ** 6, 0) == 0
@@ -208,7 +208,7 @@ def test_calls_run_on_the_caches_device_and_its_stream(monkeypatch, current):
     meta = torch.device("meta")
     c = object.__new__(et.KVCache)
     c.device, c.fmt, c.head_dim, c.n_kv_heads, c._width, c._scale, c._cache, c._lib = meta, "bf16", 64, 2, 128, 0.125, None, _Lib()
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: _Device.current)
+    monkeypatch.setattr(B, "_current_device", lambda: _Device.current)
     monkeypatch.setattr(torch.cuda, "device", lambda d: _Device(d.index))
     monkeypatch.setattr(torch.cuda, "stream", lambda s: _Device(s.device.index))
     monkeypatch.setattr(B, "_raw_stream", lambda d: ("stream of", d))
