@@ -398,7 +398,7 @@ int et_kv_read(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *
  * of all sequences are shared out evenly over the chip's workgroups on the device, by the lengths it finds there, so a generous bound
  * costs little; sequences that are short by their bound are one part each.  Two equal calls give equal bits; a sequence beside
  * others, or under another bound, may be split elsewhere, which moves its result within the rounding.  Logits, their maximum, the
- * sums and the products' accumulators are float32, the weights bfloat16; values are summed before the division by the weights'
+ * sums and the products' accumulators are float32, the weights within 2^-15 of that; values are summed before the division by the weights'
  * sum, so those beyond 2^100 can overflow.  workspace: et_attention_paged_workspace_bytes with the same arguments (0 where
  * max_len is at most 512), contents arbitrary, aligned to 16 bytes; calls that run at the same time need one each.  n_seqs * n_heads
  * at most 2^24, n_seqs * max_len at most 2^36.  Asynchronous on `hip_stream`.  Errors: INVALID_ARG, UNSUPPORTED (page_size,

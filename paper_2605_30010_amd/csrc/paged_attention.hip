@@ -217,8 +217,9 @@ struct PagedMore {                                       // the kernel's argumen
 // 32 tokens in turn: logits S^T = K Q^T, weights against a running reference, O^T += V^T P^T, where the accumulators that hold S^T are,
 // exponentiated and rounded, operand B of the second product (which tokens a lane's eight places of the contraction stand for is free, and the
 // values are loaded to match).  The cache's bytes go to registers in operand order, with no LDS on the way, the next tile's keys while a
-// tile is worked on; nothing is read twice.  Weights are rounded to bfloat16 (half a step, 2^-8 of each; the values' precision is no better),
-// logits, reference, sums and accumulators are float32.
+// tile is worked on; nothing is read twice.  A weight is taken as the sum of two bfloat16 numbers (within 2^-15 of it) by two matrix
+// instructions on the same values, so that what is left of its rounding is far below the result's own, 2^-8; logits, reference, sums
+// and accumulators are float32.
 // Bound by the memory side from some 10 MB on: 537 MB of bfloat16 (one sequence of 131072 tokens, 8 key-value heads of 128) in 91 us,
 // 5.9 TB/s, 1.16 GB of e4m3 (64 sequences) in 208, 5.6 TB/s, by the counters 1.00 of these bytes; below that by the chain launch -
 // length - page - keys - products - joined wavefronts, 4.0 us at the least.  Two workgroups per compute unit are asked for: without that the compiler
@@ -374,7 +375,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
         if (!whole && (dead >> e & 1)) p[e] = 0.f;
       }
     }
-    const u32x4 pf{cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3]), cvt_pk_bf16(p[4], p[5]), cvt_pk_bf16(p[6], p[7])};
+    // The weights' halves: what bfloat16 cuts off goes into the second.  Neither is 0 or negative where the weight is not (2^-20 of it is
+    // added), so that an infinite value stays one.
+    u32x4 pf, pl;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      pf[e] = __builtin_amdgcn_perm(__float_as_uint(p[2 * e + 1]), __float_as_uint(p[2 * e]), 0x07060302u);
+      pl[e] = cvt_pk_bf16(fmaf(p[2 * e], 0x1p-20f, p[2 * e] - bf16lo_to_f32(pf[e])), fmaf(p[2 * e + 1], 0x1p-20f, p[2 * e + 1] - bf16hi_to_f32(pf[e])));
+    }
 #pragma unroll
     for (int blk = 0; blk < V::BLOCKS; ++blk) {
       if (!whole) {
@@ -384,7 +392,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
           for (int x = 0; x < V::NREG; ++x) vw[e][x] = dead >> e & 1 ? 0 : vw[e][x];     // (0 times what lies there could be NaN)
       }
 #pragma unroll
-      for (int j = 0; j < V::DPL; ++j) acc[blk * V::DPL + j] = mfma16(V::operand(vw, j), pf, acc[blk * V::DPL + j]);
+      for (int j = 0; j < V::DPL; ++j) {
+        const u32x4 values = V::operand(vw, j);
+        f32x4 &to = acc[blk * V::DPL + j];
+        to = mfma16(values, pf, mfma16(values, pl, to));
+      }
       if (blk + 1 < V::BLOCKS) load_values(blk + 1);
     }
   }
