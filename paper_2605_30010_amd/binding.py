@@ -618,21 +618,25 @@ class KVCache:
 
     def read(self, page_table, kv_len, cu_rows=None, rows=None, out=None, stream=None):
         """The last cu_rows[b + 1] - cu_rows[b] tokens of every sequence b (None: one each) as bf16 rows (k, v), [rows,
-        n_kv_heads * head_dim] each.  Rows that belong to no sequence stay as `out` = (k, v) has them."""
+        n_kv_heads * head_dim] each.  With cu_rows, `rows` is cu_rows[n_seqs], which only the caller knows here (default: all rows
+        of out).  Rows that belong to no sequence stay as `out` = (k, v) has them; without `out` they hold anything."""
         s = self._here(stream)
         if s is None:
             with self._elsewhere(stream):
                 return self.read(page_table, kv_len, cu_rows, rows, out)
         seqs = self._seqs(page_table, kv_len)
         cu = None if cu_rows is None else self._cu(cu_rows, kv_len)
-        rows = seqs.n_seqs if rows is None else int(rows)
         if out is None:
+            if rows is None and cu is not None:
+                raise ValueError("rows (or out) is needed with cu_rows")
+            rows = seqs.n_seqs if rows is None else int(rows)
             k = torch.empty(max(rows, 0), self._width, dtype=torch.bfloat16, device=self.device)
             v, k_stride, v_stride = torch.empty_like(k), self._width, self._width
             out = k, v
         else:
             k, k_rows, _, k_stride = self._rows(out[0], "out[0]", self._width)
             v, v_rows, _, v_stride = self._rows(out[1], "out[1]", self._width)
+            rows = (seqs.n_seqs if cu is None else k_rows) if rows is None else int(rows)
             if k_rows < rows or v_rows < rows:
                 raise ValueError("out has fewer than %d rows" % rows)
         _check(self._lib.et_kv_read(self._cache, seqs, cu, rows, k.data_ptr(), k_stride, v.data_ptr(), v_stride, s))
