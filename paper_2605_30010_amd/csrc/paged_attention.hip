@@ -441,10 +441,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
         for (int w = 0; w < kWaves; ++w) x[e] = fmaf(f[w], lds_o[w][d + e][h], x[e]);
       }
       if (part.count == 1) {
-        const float inv = total == 0.f ? 0.f : value_factor<FMT>() / total;
+        const float inv = value_factor<FMT>() / total;
         u32x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = cvt_pk_bf16(x[2 * e] * inv, x[2 * e + 1] * inv);
+        for (int e = 0; e < 4; ++e) v[e] = total == 0.f ? 0 : cvt_pk_bf16(x[2 * e] * inv, x[2 * e + 1] * inv);  // (0 times x could be NaN)
         *reinterpret_cast<u32x4 *>(o.out + head * HD + blk * BD + d) = v;
       } else {
         float *to = o.part_o + slot * HD + blk * BD + d;

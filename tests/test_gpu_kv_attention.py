@@ -70,3 +70,25 @@ def test_infinite_values_stay_infinite(n, bound):
         assert (got[:, 2] == np.inf).all() if w == 0 or n == 1 else np.isfinite(got[:, 2]).all()
         # (of one token alone, the last of the two that are written into it stays)
         assert np.isnan(got[:, 4]).all() if n > 1 else (got[:, 4] == -np.inf).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("n,bound", [(1, 16), (40, 40), (300, 300), (100, 5000), (700, 5000)])
+def test_heads_with_logits_of_minus_infinity_only_get_zeros_whatever_the_values(fmt, n, bound):
+    rng = np.random.default_rng(34)
+    page, d = 16, 64
+    table, n_pages = tables(rng, [n], page)
+    host = Pages(n_pages, page, 1, d, fmt, fill=0xFF)
+    for pos in range(n):
+        at = O.place(pos, table[0], n_pages, page)
+        host.put(*at, bf16(np.abs(rng.normal(size=(1, d))) + 0.5), False)
+        v = bf16(rng.normal(size=(1, d)))
+        v[0, :3] = np.inf, -np.inf, np.nan
+        host.put(*at, v, True)
+    wide = np.full((1, -(-bound // page)), -1, dtype=np.int32)
+    wide[:, :table.shape[1]] = table
+    q = bf16(np.abs(rng.normal(size=(3, d))) + 0.5)
+    q[1, 7] = -np.inf                                                 # (keys are positive: every logit of head 1 is minus infinity)
+    got = dev_to_f64(host.on_device().attend(bits_to_dev(f64_to_bits(q.reshape(1, -1))), dev(wide), dev(np.array([n], dtype=np.int32)),
+                                             bound)).reshape(3, d)
+    assert np.isnan(got[0, 2]) and np.isnan(got[2, 2]) and not got[1].any()
