@@ -380,7 +380,7 @@ typedef struct {
 size_t et_kv_page_bytes(int32_t page_size, int32_t n_kv_heads, int32_t head_dim, int32_t format);
 
 /* Store rows of k_dev and v_dev, bf16 [rows, n_kv_heads * head_dim] with row strides in elements (multiples of 8, pointers
- * aligned to 16 bytes; columns of a fused projection can be passed as they lie).  Asynchronous on `hip_stream`.  Errors:
+ * aligned to 16 bytes; columns of a fused projection can be passed as they lie); rows at most 2^30 - 64.  Asynchronous on `hip_stream`.  Errors:
  * INVALID_ARG, UNSUPPORTED (page_size, head_dim), HIP. */
 int et_kv_append(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *cu_rows_dev, int32_t rows,
                  const uint16_t *k_dev, int64_t k_stride, const uint16_t *v_dev, int64_t v_stride, void *hip_stream);
@@ -401,7 +401,7 @@ int et_kv_read(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *
  * sums and the products' accumulators are float32, the weights within 2^-15 of that; values are summed before the division by the weights'
  * sum, so those beyond 2^100 can overflow.  workspace: et_attention_paged_workspace_bytes with the same arguments (0 where
  * max_len is at most 512), contents arbitrary, aligned to 16 bytes; calls that run at the same time need one each.  n_seqs * n_heads
- * at most 2^24, n_seqs * max_len at most 2^36.  Asynchronous on `hip_stream`.  Errors: INVALID_ARG, UNSUPPORTED (page_size,
+ * at most 2^24 (2^24 - 2^19 where every query head has its own key-value head), n_seqs * max_len at most 2^36.  Asynchronous on `hip_stream`.  Errors: INVALID_ARG, UNSUPPORTED (page_size,
  * head_dim), WORKSPACE, HIP. */
 size_t et_attention_paged_workspace_bytes(const et_kv_cache *cache, const et_kv_seqs *seqs, int32_t n_heads,
                                           int32_t max_len, int32_t window);

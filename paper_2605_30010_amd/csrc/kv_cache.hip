@@ -250,11 +250,13 @@ KvPages kv_pages(const et_kv_cache &c) {
   return {static_cast<char *>(c.data_dev), (int64_t)et_kv_page_bytes(c.page_size, c.n_kv_heads, c.head_dim, c.format), c.n_pages,
           __builtin_ctz(c.page_size), c.n_kv_heads};
 }
+// A launch takes fewer than 2^32 lanes, 256 a workgroup, and a workgroup at most 64 rows.
+constexpr int kMaxBlocks = (1 << 24) - 1, kMaxRows = 64 * kMaxBlocks;
 static int check_rows(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *cu, int rows, const void *k, int64_t k_stride,
                       const void *v, int64_t v_stride) {
   int rc;
   if ((rc = check_kv(cache, seqs))) return rc;
-  ET_REQUIRE(rows >= 0 && rows <= 1 << 30, "rows = %d must be in [0, 2^30]", rows);
+  ET_REQUIRE(rows >= 0 && rows <= kMaxRows, "rows = %d must be in [0, 2^30 - 64]", rows);
   ET_REQUIRE(cu || rows == seqs->n_seqs, "rows = %d without cu_rows_dev must be n_seqs = %d", rows, seqs->n_seqs);
   if (rows == 0) return ET_OK;
   const int64_t width = (int64_t)cache->n_kv_heads * cache->head_dim;
@@ -271,7 +273,8 @@ static int check_rows(const et_kv_cache *cache, const et_kv_seqs *seqs, const in
 // rows: 928 000 int8 rows of 3 heads of 64 read 293 / 261 / 251, 630 000 of one head of 128 stored and read back 259 / 222 / 220.
 static int rows_per_block(int rows, const et_kv_cache &c) {
   const int lanes = c.head_dim <= 64 ? 8 : c.head_dim <= 128 ? 16 : 32, turns = c.format == ET_KV_BF16 ? 4 : 16;
-  return std::max(1, std::min({64, rows / 1024, turns * (256 / lanes) / (2 * c.n_kv_heads)}));
+  const int least = (int)(((int64_t)rows + kMaxBlocks - 1) / kMaxBlocks);
+  return std::max(least, std::min({64, rows / 1024, turns * (256 / lanes) / (2 * c.n_kv_heads)}));
 }
 
 template <bool STORE>

@@ -565,6 +565,10 @@ static int check_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, int n_h
   ET_REQUIRE((int64_t)seqs->n_seqs * n_heads <= 1 << 24, "n_seqs * n_heads = %lld is above 2^24", (long long)seqs->n_seqs * n_heads);
   ET_REQUIRE((int64_t)seqs->n_seqs * std::min(max_len, seqs->pages_per_seq * cache->page_size) <= 1ll << 36,
              "n_seqs * max_len is above 2^36");
+  // (a launch takes fewer than 2^32 lanes)
+  const PagedPlan p = paged_plan(*cache, *seqs, n_heads, max_len, window);
+  ET_REQUIRE(p.items * p.units < (1ll << 32) / (64 * kWaves), "n_seqs * n_kv_heads = %lld is too much for one launch",
+             (long long)seqs->n_seqs * cache->n_kv_heads);
   return ET_OK;
 }
 
