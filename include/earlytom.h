@@ -396,7 +396,7 @@ int et_kv_read(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *
  * head_dim] with row stride q_stride (a multiple of 8; aligned to 16 bytes); out_dev bf16 [n_seqs, n_heads * head_dim],
  * contiguous, not q_dev.  max_len: a bound of every kv_len that the host knows (positions from max_len on are left out).  The tokens
  * of all sequences are shared out evenly over the chip's workgroups on the device, by the lengths it finds there, so a generous bound
- * costs little; sequences that are short by their bound are one part each.  Two equal calls give equal bits; a sequence beside
+ * costs little; sequences that are short by their bound, or more than 4096, are one part each.  Two equal calls give equal bits; a sequence beside
  * others, or under another bound, may be split elsewhere, which moves its result within the rounding.  Logits, their maximum, the
  * sums and the products' accumulators are float32, the weights within 2^-15 of that; values are summed before the division by the weights'
  * sum, so those beyond 2^100 can overflow.  workspace: et_attention_paged_workspace_bytes with the same arguments (0 where

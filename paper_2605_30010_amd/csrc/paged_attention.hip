@@ -546,8 +546,11 @@ static PagedPlan paged_plan(const et_kv_cache &c, const et_kv_seqs &s, int n_hea
   // One part each where that is as fast: short sequences, and longer ones that fill the chip by themselves.  us as one part / shared out:
   // 1 x 197 tokens 4.7 / 6.7, 256 x 500 of 4 key-value heads 52 / 63, 4 x 1000 of 32 14.5 / 17.0, 1024 x 100 to 2048 of 4 220 / 275; but
   // 1 x 700 of 8 10.2 / 7.8, 4 x 1500 of 4 16.1 / 9.2, 64 x 1000 to 16384 of 8 256 / 214.
+  // Beyond 4096 sequences too: every workgroup of a call that is shared out looks at all lengths, which would come to a minute for
+  // a million sequences.  us as one part / shared out, bound 131072: 4097 x 60 tokens of 8 195 / 1200, 0 to 8000 8768 / 9167, 60 with one of
+  // 131072 among them 1419 / 1261 (of one key-value head 1113 / 277).
   const int64_t all = (int64_t)s.n_seqs * p.units;
-  const bool whole = span <= 512 || (span <= 1024 && all >= 64) || (span <= 2048 && all >= 1024);
+  const bool whole = span <= 512 || (span <= 1024 && all >= 64) || (span <= 2048 && all >= 1024) || s.n_seqs > 4096;
   p.share = whole ? 0 : (int)std::min<int64_t>(blocks, (kShare + p.units - 1) / p.units);
   p.items = p.share * (s.n_seqs > 1 ? kFiner : 1) + (int64_t)s.n_seqs;
   p.slots = p.share ? (size_t)p.items * n_heads : 0;

@@ -130,3 +130,12 @@ def test_rows_launch_what_they_accept(ask):
             assert code == 0 and 0 < lanes < 2 ** 32 and launches == 2, c
         else:
             assert code == -1 and launches == 0, c
+
+
+def test_many_sequences_are_one_part_each(ask):
+    """Where a call is shared out, every workgroup looks at all lengths: not with any number of sequences."""
+    calls = [("attend", kv, heads, 64, seqs, bound, 0) for kv, heads in ((1, 1), (1, 8), (8, 32)) for seqs in (4097, 2 ** 16, 2 ** 19)
+             for bound in (2049, 2 ** 17)]
+    for c, (code, lanes, launches, bytes) in zip(calls, ask(calls)):
+        assert code == 0 and launches == 1 and bytes == 0 and lanes == c[1] * c[4] * 256, c
+    assert all(r[2] == 2 and r[3] > 0 for r in ask([("attend", 1, 8, 64, seqs, 4000, 0) for seqs in (2, 1000, 4096)]))
