@@ -569,6 +569,7 @@ class Projector:
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
+_INT_MAX = 2 ** 31 - 1
 _KV_FORMATS = {"bf16": ET_KV_BF16, "e4m3": ET_KV_E4M3, "int8": ET_KV_INT8}
 
 
@@ -654,7 +655,7 @@ class KVCache:
         seqs, lib = self._seqs(page_table, kv_len), self._lib
         if n != seqs.n_seqs:
             raise ValueError("q has %d rows for %d sequences" % (n, seqs.n_seqs))
-        heads, max_len, window = width // self.head_dim, int(max_len), int(window)
+        heads, max_len, window = width // self.head_dim, min(int(max_len), _INT_MAX), min(int(window), _INT_MAX)
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif _dev(out, torch.bfloat16, "out").numel() != n * width or out.device != self.device:

@@ -61,3 +61,13 @@ def test_read_of_row_ranges_takes_all_rows_of_out_or_asks_for_their_number(cache
     with pytest.raises(ValueError, match="rows"):
         cache.read(tab, lens, cu, out=(rows(40), rows(39)))
     assert len(cache._lib.calls) == n
+
+
+@pytest.mark.parametrize("max_len,window", [(2 ** 31, 0), (2 ** 32 + 16, 2 ** 32 + 5), (2 ** 63 - 1, 2 ** 31), (10 ** 30, 2 ** 32), (600, 7), (16, 0)])
+def test_bounds_and_windows_past_32_bits_are_bounds_and_windows(cache, max_len, window):
+    """No length reaches 2^31: a larger bound or window is the same as the largest, and not its low bits."""
+    cache.attend(rows(3, 256), ints(3, 2), ints(3), max_len, window=window)
+    name, args = cache._lib.calls[-1]
+    assert name == "et_attention_paged" and args[5:7] == (min(max_len, 2 ** 31 - 1), min(window, 2 ** 31 - 1))
+    asked = [a for n, a in cache._lib.calls if n == "et_attention_paged_workspace_bytes"]
+    assert all(a[3:5] == args[5:7] for a in asked) and len(asked) == (max_len > 512)
