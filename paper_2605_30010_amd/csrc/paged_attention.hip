@@ -10,8 +10,8 @@ namespace et {
 constexpr int kTile = 32;                                // tokens that a wavefront takes at a time
 constexpr int kWaves = 4;                                // wavefronts of a workgroup
 constexpr int kBlock = kWaves * kTile;
-// Workgroups that a call is shared out over: two per compute unit (us at 512 / 768 / 1024: 32 x 0 to 5309 int8 tokens 22.6 / 23.2 / 26.0,
-// 131072 bfloat16 tokens 95 / 96 / 97); and how many times as many at most (see part_blocks).
+// Workgroups that a call is shared out over: two per compute unit (us at 512 / 768 / 1024: 32 x 0 to 5309 int8 tokens 21.9 / 23.2 / 25.0,
+// 131072 bfloat16 tokens 96 / 98 / 97); and how many times as many at most (see part_blocks).
 constexpr int kShare = 512, kFiner = 4;
 
 // a * b rounded, never part of a fused multiply-add: a logit less the maximum has to be 0 for the maximum itself, however large.
@@ -40,7 +40,7 @@ struct SeqRange {
   __device__ __forceinline__ uint32_t blocks() const { return hi > lo ? (uint32_t)(hi - lo + kBlock - 1) / kBlock : 0; }
 };
 // Blocks of a part.  Sequences seldom end with a whole part, so where there are several and the parts are long, shorter ones even
-// out what the last parts leave over: 64 x 1000 to 16384 e4m3 tokens 241 -> 214 us, 12 x 2000 to 8000 with heads of 256 115 -> 100.
+// out what the last parts leave over: 64 x 1000 to 16384 e4m3 tokens 247 -> 215 us, 12 x 2000 to 8000 with heads of 256 116 -> 101.
 __device__ __forceinline__ uint32_t part_blocks(const PagedArgs &a, uint32_t total) {
   const uint32_t per = max((total + a.share - 1) / a.share, 1u);
   return a.n_seqs > 1 && per > 8 ? max((per + kFiner - 1) / kFiner, 8u) : per;
@@ -217,14 +217,14 @@ struct PagedMore {                                       // the kernel's argumen
 // 32 tokens in turn: logits S^T = K Q^T, weights against a running reference, O^T += V^T P^T, where the accumulators that hold S^T are,
 // exponentiated and rounded, operand B of the second product (which tokens a lane's eight places of the contraction stand for is free, and the
 // values are loaded to match).  The cache's bytes go to registers in operand order, with no LDS on the way, the next tile's keys while a
-// tile is worked on; nothing is read twice.  A weight is taken as the sum of two bfloat16 numbers (within 2^-15 of it) by two matrix
-// instructions on the same values, so that what is left of its rounding is far below the result's own, 2^-8; logits, reference, sums
-// and accumulators are float32.
+// tile is worked on; up to 16 query heads per key-value head read everything once, more of them once for each 16.  A weight is taken as
+// the sum of two bfloat16 numbers (within 2^-15 of it) by two matrix instructions on the same values, so that what is left of its
+// rounding is far below the result's own, 2^-8; logits, reference, sums and accumulators are float32.
 // Bound by the memory side from some 10 MB on: 537 MB of bfloat16 (one sequence of 131072 tokens, 8 key-value heads of 128) in 91 us,
-// 5.9 TB/s, 1.16 GB of e4m3 (64 sequences) in 208, 5.6 TB/s, by the counters 1.00 of these bytes; below that by the chain launch -
-// length - page - keys - products - joined wavefronts, 4.0 us at the least.  Two workgroups per compute unit are asked for: without that the compiler
-// moves the accumulators to and fro between the two halves of the registers, and 32 int8 sequences of up to 5309 tokens take 23.4
-// instead of 21.6 us, 12 of 2000 to 8000 with 16 heads of 256 119 instead of 100.
+// 5.9 TB/s, 1.16 GB of e4m3 (64 sequences) in 209, 5.6 TB/s, by the counters 1.00 of these bytes; below that by the chain launch -
+// length - page - keys - products - joined wavefronts, 4.1 us at the least.  Two workgroups per compute unit are asked for: without that the compiler
+// moves the accumulators to and fro between the two halves of the registers, and 32 int8 sequences of up to 5309 tokens take 24.0
+// instead of 21.9 us, 12 of 2000 to 8000 with 16 heads of 256 134 instead of 101.
 template <int HD, int FMT, bool ONE>
 __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const int32_t *len, const int32_t *table, int n_seqs,
                                                                       int share, int bound, int window, int units, int row_tiles,
@@ -381,7 +381,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       pf[e] = __builtin_amdgcn_perm(__float_as_uint(p[2 * e + 1]), __float_as_uint(p[2 * e]), 0x07060302u);
-      pl[e] = cvt_pk_bf16(fmaf(p[2 * e], 0x1p-20f, p[2 * e] - bf16lo_to_f32(pf[e])), fmaf(p[2 * e + 1], 0x1p-20f, p[2 * e + 1] - bf16hi_to_f32(pf[e])));
+      pl[e] = cvt_pk_bf16(fmaf(p[2 * e], 0x1p-20f, p[2 * e] - bf16lo_to_f32(pf[e])),
+                          fmaf(p[2 * e + 1], 0x1p-20f, p[2 * e + 1] - bf16hi_to_f32(pf[e])));
     }
 #pragma unroll
     for (int blk = 0; blk < V::BLOCKS; ++blk) {
@@ -459,7 +460,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
 // Joins the parts of one query head, always in the same order: groups of lanes, four dimensions a lane, take every GROUPS-th part
 // with a running maximum and sum, eight parts' loads in flight, and the groups' results are added up in the groups' order.
 // A head whose sequence is one part has its result already.  THREADS: 64 where a sequence has few parts.  Bound by latency: 28 heads of
-// 40 parts take 3.2 us, 32 of 64 4.5, 2048 of four 4.9.
+// 40 parts take 3.1 us, 32 of 64 5.0, 2048 of four 5.1.
 template <int HD, int FMT, int THREADS, bool ONE>
 __global__ __launch_bounds__(THREADS) void paged_join_kernel(const int32_t *len, const float *part_o, const float2 *part_ml, int n_seqs,
                                                              int share, int bound, int window, int n_heads, uint16_t *out) {
@@ -544,11 +545,13 @@ static PagedPlan paged_plan(const et_kv_cache &c, const et_kv_seqs &s, int n_hea
   const int span = window > 0 ? (int)std::min<int64_t>(p.bound, (int64_t)window + 15) : p.bound;
   const int64_t blocks = (int64_t)s.n_seqs * ((span + kBlock - 1) / kBlock);
   // One part each where that is as fast: short sequences, and longer ones that fill the chip by themselves.  us as one part / shared out:
-  // 1 x 197 tokens 4.7 / 6.7, 256 x 500 of 4 key-value heads 52 / 63, 4 x 1000 of 32 14.5 / 17.0, 1024 x 100 to 2048 of 4 220 / 275; but
-  // 1 x 700 of 8 10.2 / 7.8, 4 x 1500 of 4 16.1 / 9.2, 64 x 1000 to 16384 of 8 256 / 214.
+  // 1 x 197 tokens 4.8 / 7.7, 256 x 500 of 4 key-value heads 50 / 58, 4 x 1000 of 32 13.7 / 16.7, 1024 x 100 to 2048 of 4 223 / 261;
+  // but 1 x 700 of 8 10.0 / 7.8, 4 x 1500 of 4 16.8 / 8.6, 64 x 1000 to 16384 of 8 255 / 215.  The host knows the bound only, so a
+  // generous one takes the second figure; and the rule counts tokens, not their bytes (64 x 1024 of one bfloat16 head of 256, one part
+  // each: 24.0 / 20.3).
   // Beyond 4096 sequences too: every workgroup of a call that is shared out looks at all lengths, which would come to a minute for
-  // a million sequences.  us as one part / shared out, bound 131072: 4097 x 60 tokens of 8 195 / 1200, 0 to 8000 8768 / 9167, 60 with one of
-  // 131072 among them 1419 / 1261 (of one key-value head 1113 / 277).
+  // a million sequences.  Bound 131072: 4097 x 60 tokens of 8 195 / 1200, 0 to 8000 8768 / 9167, 60 with one of 131072 among them
+  // 1419 / 1261 (of one key-value head 1113 / 277).
   const int64_t all = (int64_t)s.n_seqs * p.units;
   const bool whole = span <= 512 || (span <= 1024 && all >= 64) || (span <= 2048 && all >= 1024) || s.n_seqs > 4096;
   p.share = whole ? 0 : (int)std::min<int64_t>(blocks, (kShare + p.units - 1) / p.units);
