@@ -92,3 +92,32 @@ def test_heads_with_logits_of_minus_infinity_only_get_zeros_whatever_the_values(
     got = dev_to_f64(host.on_device().attend(bits_to_dev(f64_to_bits(q.reshape(1, -1))), dev(wide), dev(np.array([n], dtype=np.int32)),
                                              bound)).reshape(3, d)
     assert np.isnan(got[0, 2]) and np.isnan(got[2, 2]) and not got[1].any()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("lens", [[40, 3], [1500, 900]])
+@pytest.mark.parametrize("q_exp,k_exp,v_exp", [(0, 0, -88), (0, 0, 97), (95, -95, 0), (-95, 95, 0)])
+def test_sizes_up_to_the_stated_limits(fmt, lens, q_exp, k_exp, v_exp):
+    """Queries and values up to 2^100, value rows down to 2^-90; the bound is that of the weights' test (all sizes are powers of
+    two times ordinary ones, and nothing leaves the range of normal float32 numbers)."""
+    rng = np.random.default_rng(35)
+    page, kv, heads, d = 32, 1, 6, 64
+    table, n_pages = tables(rng, lens, page)
+    host = Pages(n_pages, page, kv, d, fmt, fill=0xFF)
+    tokens = []
+    for b, n in enumerate(lens):
+        rows = [], []
+        for pos in range(n):
+            at = O.place(pos, table[b], n_pages, page)
+            for j, e in ((0, k_exp), (1, v_exp)):
+                host.put(*at, bf16(np.clip(rng.normal(size=(kv, d)), -4, 4)) * 2.0 ** e, bool(j))
+                rows[j].append(host.get(*at, bool(j)))
+        tokens.append([np.array(r) for r in rows])
+    q = bf16(np.clip(rng.normal(size=(len(lens), heads, d)), -4, 4)) * 2.0 ** q_exp
+    got = dev_to_f64(host.on_device().attend(bits_to_dev(f64_to_bits(q.reshape(len(lens), -1))), dev(table),
+                                             dev(np.array(lens, dtype=np.int32)), max(lens))).reshape(q.shape)
+    for b, n in enumerate(lens):
+        ref, mass, size = O.attend_one(q[b], *tokens[b], 1.0 / math.sqrt(d))
+        rest = (2.0 ** -15 + 2.0 ** -20 + 2 * (d + 8) * 2.0 ** -24 * 1.45 * size[:, None] + 2 * n * 2.0 ** -24 + 2.0 ** -21) * mass
+        off = np.abs(got[b] - ref) - (2.0 ** -8 * np.abs(ref) + 1.01 * rest)
+        assert (off <= 0).all(), (b, n, float((off / mass).max()), int((off > 0).sum()), off.size)
