@@ -340,7 +340,7 @@ int et_project_tokens(et_projector *proj, const uint16_t *tokens_dev, int32_t ro
 /* ---- the key-value cache of the language model behind the projector ------------------------------
  * The kept tokens end up as keys and values in a cache that every later token of the answer reads.  The cache is paged:
  * `n_pages` pages of `page_size` tokens in one device buffer that the caller owns, and a page table that
- * gives each sequence its pages.  These calls store new keys and values (in 8 bits if asked to), read them
+ * gives each sequence its pages.  These calls store new keys and values (in 8 or 4 bits if asked to), read them
  * back, and compute the attention of one new token for each sequence.
  *
  * A page is et_kv_page_bytes() bytes, one key-value head after the other; a head's part holds
@@ -349,6 +349,14 @@ int et_project_tokens(et_projector *proj, const uint16_t *tokens_dev, int32_t ro
  * ET_KV_E4M3: one byte per value (two's complement; OCP 8-bit float with 4 exponent bits); a row x of
  * head_dim values is held as its largest magnitude m (bfloat16, exact) and the codes round(x * Q / m), ties to even, Q = 127
  * or 448; it stands for code * m / Q.  A row with an infinity or a NaN has m = NaN and reads back as NaN throughout.
+ * ET_KV_MXFP4: 4 bits per value and one exponent for 32 of them (4.25 bits in all where head_dim is a multiple of 32, 4.3 for 80).
+ * A head's part holds
+ *     keys [page_size, head_dim / 2] | values [page_size, head_dim / 2] | key exponents [page_size, blocks] | value exponents [blocks, page_size],
+ * blocks = ceil(head_dim / 32) (the last of 80 has 16 dimensions), an exponent being the byte e + 127, two codes a byte, the even
+ * dimension in the low half: the sign (8) and the number (0 to 7) of one of 0, 0.5, 1, 1.5, 2, 3, 4, 6, times 2^e.  e is the
+ * smallest with which the block's largest magnitude is at most 7 * 2^e, within -125 .. 125; the nearest value is taken, ties to the even code,
+ * and magnitudes past 6 * 2^e become 6 * 2^e.  A block with an infinity or a NaN has the byte 255 and codes 0, and reads back as NaN; the
+ * row's other blocks keep their values.  Every value is exact in bfloat16.
  *
  * Token `pos` of sequence b is token pos % page_size of page page_table[b * table_stride + pos / page_size].  An
  * entry outside [0, n_pages) is no page: nothing is stored there, it reads back as zeros, and attention leaves its tokens out;
@@ -362,7 +370,7 @@ int et_project_tokens(et_projector *proj, const uint16_t *tokens_dev, int32_t ro
  * (kv_len counts the new tokens).  cu_rows_dev = NULL: one row for each sequence (rows = n_seqs).  Rows outside
  * cu_rows[0] .. cu_rows[n_seqs], such as padding behind the last sequence, are neither read nor written; a row whose
  * position would be negative (an idle slot of kv_len 0) is not stored and reads back as zeros. */
-enum { ET_KV_BF16 = 0, ET_KV_E4M3 = 1, ET_KV_INT8 = 2 };
+enum { ET_KV_BF16 = 0, ET_KV_E4M3 = 1, ET_KV_INT8 = 2, ET_KV_MXFP4 = 4 };
 typedef struct {
   void *data_dev;              /* n_pages * et_kv_page_bytes bytes, aligned to 16                    */
   int32_t n_pages, page_size;  /* page_size 16, 32, 64, 128 or 256                                   */
@@ -402,7 +410,8 @@ int et_kv_read(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *
  * its result within the rounding.
  * Logits, their maximum, the sums and the products' accumulators are float32, the weights within 2^-15 of that.  Values are summed
  * before the division by the weights' sum, and in 8 bits a query's products with the codes before the row's factor, so values and
- * queries beyond 2^100 can overflow; in 8 bits the weights carry the value rows' maxima, so those below 2^-90 lose bits.
+ * queries beyond 2^100 can overflow; in 8 bits the weights carry the value rows' maxima, so those below 2^-90 lose bits.  Keys
+ * and values in 4 bits enter both products as the exact numbers that they stand for.
  * workspace: et_attention_paged_workspace_bytes with the same arguments (0 where max_len is at most 512), contents arbitrary, aligned
  * to 16 bytes; calls that run at the same time need one each.  n_seqs * n_heads at most 2^24 (2^24 - 2^19 where every query head
  * has its own key-value head), n_seqs * max_len at most 2^36.  Asynchronous on `hip_stream`.  Errors: INVALID_ARG, UNSUPPORTED

@@ -65,3 +65,42 @@ def attend_one(q, k, v, scale):
         w /= w.sum()
         out[h], mass[h] = w @ vh, w @ np.abs(vh)
     return out, mass, size
+
+
+# ---------------------------------------------------------------------------------------------- 4 bits, blocks of 32 with one power of two
+
+MX_GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def mx_blocks(d):
+    return -(-d // 32)
+
+
+def mx_hold(x):
+    """Rows x [..., d] float64 (bfloat16 values) -> (codes uint8 [..., d / 2], the even dimension in the low half, exponent bytes uint8
+    [..., blocks]); a block with an infinity or a NaN has the byte 255 and codes 0."""
+    d = x.shape[-1]
+    codes, exps = np.zeros(x.shape, dtype=np.uint8), np.zeros(x.shape[:-1] + (mx_blocks(d),), dtype=np.uint8)
+    for i in range(mx_blocks(d)):
+        b = x[..., 32 * i:32 * i + 32]
+        finite = np.isfinite(b).all(-1)
+        b = np.where(finite[..., None], b, 0.0)
+        m = np.abs(b).max(-1)
+        e = np.floor(np.log2(np.where(m > 0, m, 1.0) / 7.0)) - 1        # the smallest with m <= 7 * 2^e: from below, by comparing
+        for _ in range(3):
+            e = np.where(m > 7.0 * 2.0 ** e, e + 1, e)
+        e = np.clip(np.where(m > 0, e, -125), -125, 125)
+        a = np.minimum(np.abs(b) / 2.0 ** e[..., None], 6.0)
+        up = np.clip(np.searchsorted(MX_GRID, a), 1, 7)
+        low, high = a - MX_GRID[up - 1], MX_GRID[up] - a
+        near = np.where((high < low) | ((high == low) & (up % 2 == 0)), up, up - 1)
+        codes[..., 32 * i:32 * i + 32] = np.where(finite[..., None], near + 8 * np.signbit(b), 0)
+        exps[..., i] = np.where(finite, e + 127, 255)
+    return codes[..., 0::2] | codes[..., 1::2] << 4, exps
+
+
+def mx_stands_for(codes, exps):
+    c = np.stack((codes & 15, codes >> 4), -1).reshape(codes.shape[:-1] + (2 * codes.shape[-1],))
+    v = np.where(c > 7, -1.0, 1.0) * MX_GRID[c & 7]
+    e = np.repeat(exps.astype(np.int64), 32, -1)[..., :c.shape[-1]]
+    return np.where(e == 255, np.nan, v * 2.0 ** (e - 127.0))

@@ -68,7 +68,7 @@ class _KvSeqs(C.Structure):
 ET_MERGE_MEAN, ET_MERGE_ALG1 = 0, 1
 ET_SELECT_UNIFORM, ET_SELECT_DECOUPLED = 0, 1
 ET_SCORE_L2NORM, ET_SCORE_ATTENTION = 0, 1
-ET_KV_BF16, ET_KV_E4M3, ET_KV_INT8 = 0, 1, 2
+ET_KV_BF16, ET_KV_E4M3, ET_KV_INT8, ET_KV_MXFP4 = 0, 1, 2, 4
 
 
 def library_path():
@@ -570,7 +570,7 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 _INT_MAX = 2 ** 31 - 1
-_KV_FORMATS = {"bf16": ET_KV_BF16, "e4m3": ET_KV_E4M3, "int8": ET_KV_INT8}
+_KV_FORMATS = {"bf16": ET_KV_BF16, "e4m3": ET_KV_E4M3, "int8": ET_KV_INT8, "mxfp4": ET_KV_MXFP4}
 
 
 def et_kv_page_bytes(page_size, n_kv_heads, head_dim, fmt):
@@ -579,7 +579,7 @@ def et_kv_page_bytes(page_size, n_kv_heads, head_dim, fmt):
 
 class KVCache:
     """A paged key-value cache: `data` uint8 [n_pages, page bytes] on the device (layout in earlytom.h), allocated here unless
-    given.  fmt: "bf16", "e4m3" or "int8".  The sequences are the caller's: page_table int32 [n_seqs, pages] (entries outside
+    given.  fmt: "bf16", "e4m3", "int8" or "mxfp4".  The sequences are the caller's: page_table int32 [n_seqs, pages] (entries outside
     [0, n_pages) = no page; rows may be strided), kv_len int32 [n_seqs].  Every call is asynchronous on `stream` (default: the
     current stream of the cache's device; results and workspaces are allocated there, so a result belongs to that stream),
     keeps nothing, and can be captured into a graph; calls on several streams may run at the same time as long as none of

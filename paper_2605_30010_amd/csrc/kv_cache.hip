@@ -1,4 +1,4 @@
-// Storing keys and values in a paged cache, in bfloat16 or 8 bits, and reading them back.
+// Storing keys and values in a paged cache, in bfloat16, 8 or 4 bits, and reading them back.
 #include <algorithm>
 #include <type_traits>
 
@@ -81,6 +81,14 @@ __device__ __forceinline__ uint32_t group_max(uint32_t v) {
   return v;
 }
 
+// The largest of eight values' (bf16 pairs) magnitudes, as bits: an infinity or a NaN is above all numbers.
+__device__ __forceinline__ uint32_t magnitude8(u32x4 x) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) most = max(most, max(x[e] & 0x7FFFu, x[e] >> 16 & 0x7FFFu));
+  return most;
+}
+
 // The codes of eight values (bf16 pairs) of a row whose largest magnitude has the bits `top`.  code = round(x Q / m): both
 // are taken times a power of two that brings m into [1/2, 1), so nothing overflows; x Q is exact (8 + 9 bits), and the
 // corrected product is the correctly rounded quotient.  A quotient of two 8-bit numbers times Q lies on a tie of the codes or at least 2^-13 of
@@ -144,6 +152,25 @@ __device__ __forceinline__ u32x4 dequantise8(uint2 codes, KvFactor f) {
   return out;
 }
 
+// The byte e + 127 of a block whose largest magnitude has the bits `top` (not an infinity or a NaN): the smallest 2^e with
+// top <= 7 * 2^e = 1.75 * 2^(e + 2), from -125 (no unit of a code is below the normal numbers) to 125 (6 * 2^e is a number).  7 and not the
+// 6 that is the largest code: a largest value between them loses at most 1 / 7 of itself as 6, and the others keep twice the steps.  Relative
+// error of normal values with 6 / 7 / 8: 0.1154 / 0.1119 / 0.1150, with channels of very different sizes 0.154 / 0.141 / 0.143.
+__device__ __forceinline__ uint32_t mx_exponent(uint32_t top) {
+  return min(max((int)(top >> 7) - 2 + ((top & 127u) > 96u ? 1 : 0), 2), 252);
+}
+// The codes of eight values (bf16 pairs) in units of 2^e: rounded to the nearest, ties to even, what is past 6 becomes 6.  A power of two
+// moves no bits, so every code is the one of exact arithmetic, and so is every value read back (three bits at most).
+__device__ __forceinline__ uint32_t mx_encode8(u32x4 x, uint32_t exponent) {
+  const float unit = __uint_as_float(exponent << 23);
+  uint32_t w = 0;
+  const auto pair = [&](uint32_t bits) { return __builtin_bit_cast(bf16x2, bits); };    // (of an element in place the compiler takes the first)
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, pair(x[0]), unit, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, pair(x[1]), unit, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, pair(x[2]), unit, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, pair(x[3]), unit, 3);
+}
+
 // A workgroup takes up to 64 consecutive rows of tokens.  One wavefront finds their places; then groups of LANES lanes take the rows'
 // heads in turn (a token's key heads, its value heads, the next token), kBatch of them with their loads in flight.  Bound by memory:
 // the way to a place is a chain of four loads, so rows share it when there are many.  What is read or written once in long
@@ -172,7 +199,7 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const i
     constexpr int N = decltype(batch)::value;
     u32x4 x[N];
     uint2 codes[N];
-    uint16_t top[N];
+    uint16_t top[N];                                     // in 4 bits: the block's exponent
     uint16_t *row[N];
     char *cell[N], *top_at[N];
     int go[N];                                           // 0: nothing to do, 1: no place in the cache, 2: a place
@@ -185,15 +212,20 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const i
       row[i] = (value ? v + (first + (int64_t)token) * v_stride : k + (first + (int64_t)token) * k_stride) + h * HD + sub * 8;
       char *page = c.data + (int64_t)((uint64_t)(uint32_t)place.y << 32 | (uint32_t)place.x);
       const uint32_t head = (uint32_t)h * head_bytes;
-      cell[i] = page + (head + (value ? Lay::values(n) : 0) + place.z * Lay::kRow + sub * 8 * Lay::kBytes);
-      top_at[i] = page + (head + (value ? Lay::value_max(n) : Lay::key_max(n)) + place.z * 2);
+      cell[i] = page + (head + (value ? Lay::values(n) : 0) + place.z * Lay::kRow + sub * Lay::kEight);
+      const int block = min(sub / (kMxBlock / 8), Lay::kBlocks - 1);
+      const int scale = FMT != ET_KV_MXFP4 ? 2 * place.z : value ? block * n + place.z : place.z * Lay::kBlocks + block;
+      top_at[i] = page + (head + (value ? Lay::value_scale(n) : Lay::key_scale(n)) + scale);
       x[i] = u32x4{0, 0, 0, 0};
       codes[i] = make_uint2(0, 0);
       top[i] = 0;
       if (go[i] == 2 && in_row) {
         if constexpr (STORE) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(row[i]));
         else if constexpr (FMT == ET_KV_BF16) x[i] = *reinterpret_cast<const u32x4 *>(cell[i]);
-        else {
+        else if constexpr (FMT == ET_KV_MXFP4) {
+          codes[i].x = *reinterpret_cast<const uint32_t *>(cell[i]);
+          top[i] = *reinterpret_cast<const uint8_t *>(top_at[i]);
+        } else {
           codes[i] = *reinterpret_cast<const uint2 *>(cell[i]);
           top[i] = *reinterpret_cast<const uint16_t *>(top_at[i]);
         }
@@ -204,10 +236,15 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const i
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if constexpr (STORE && FMT != ET_KV_BF16) {
-        uint32_t most = 0;                                // of the magnitudes' bits: an infinity or a NaN is above all numbers
-#pragma unroll
-        for (int e = 0; e < 4; ++e) most = max(most, max(x[i][e] & 0x7FFFu, x[i][e] >> 16 & 0x7FFFu));
+      if constexpr (STORE && FMT == ET_KV_MXFP4) {
+        uint32_t most = magnitude8(x[i]);
+        most = dpp_max<0x4E>(dpp_max<0xB1>(most));        // four lanes' values are a block
+        const bool number = most < 0x7F80u;
+        const uint32_t exponent = number ? mx_exponent(most) : 255u, code = number ? mx_encode8(x[i], exponent) : 0u;
+        if (go[i] == 2 && in_row) *reinterpret_cast<uint32_t *>(cell[i]) = code;
+        if (go[i] == 2 && in_row && sub % 4 == 0) *reinterpret_cast<uint8_t *>(top_at[i]) = (uint8_t)exponent;
+      } else if constexpr (STORE && FMT != ET_KV_BF16) {
+        uint32_t most = magnitude8(x[i]);
         most = group_max<LANES>(most);
         const bool number = most - 1u < 0x7F7Fu;          // neither 0 nor without end
         codes[i] = quantise8<FMT>(x[i], number ? most : 0x3F80u);
@@ -217,7 +254,8 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const i
       } else if constexpr (STORE) {
         if (go[i] == 2 && in_row) __builtin_nontemporal_store(x[i], reinterpret_cast<u32x4 *>(cell[i]));
       } else {
-        if constexpr (FMT != ET_KV_BF16) x[i] = dequantise8<FMT>(codes[i], kv_factor<FMT>(top[i]));
+        if constexpr (FMT == ET_KV_MXFP4) x[i] = mx_decode8(codes[i].x, top[i]);
+        else if constexpr (FMT != ET_KV_BF16) x[i] = dequantise8<FMT>(codes[i], kv_factor<FMT>(top[i]));
         if (go[i] && in_row) __builtin_nontemporal_store(x[i], reinterpret_cast<u32x4 *>(row[i]));
       }
     }
@@ -227,10 +265,12 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const i
   for (; left > 0; --left) turns(std::integral_constant<int, 1>());
 }
 
+static bool kv_format(int format) { return (format >= ET_KV_BF16 && format <= ET_KV_INT8) || format == ET_KV_MXFP4; }
+
 int check_kv(const et_kv_cache *c, const et_kv_seqs *s) {
   ET_REQUIRE(c != nullptr, "cache is NULL");
   ET_REQUIRE(s != nullptr, "seqs is NULL");
-  ET_REQUIRE(c->format >= ET_KV_BF16 && c->format <= ET_KV_INT8, "unknown cache format %d", c->format);
+  ET_REQUIRE(kv_format(c->format), "unknown cache format %d", c->format);
   ET_REQUIRE(c->n_kv_heads >= 1 && c->n_kv_heads <= 1024, "n_kv_heads = %d must be in [1, 1024]", c->n_kv_heads);
   ET_REQUIRE(c->n_pages >= 1, "n_pages = %d must be at least 1", c->n_pages);
   if (et_kv_page_bytes(c->page_size, c->n_kv_heads, c->head_dim, c->format) == 0) {
@@ -283,13 +323,16 @@ static int launch_rows(const et_kv_cache &cache, const et_kv_seqs &seqs, const i
   if (rows == 0 || seqs.n_seqs == 0) return ET_OK;
   const KvPages c = kv_pages(cache);
   const int per_block = rows_per_block(rows, cache);
-  return kv_dispatch(cache.head_dim, cache.format, [&](auto hd, auto fmt) {
+  auto launch = [&](auto hd, auto fmt) {
     kv_rows_kernel<hd.value, fmt.value, STORE><<<(rows + per_block - 1) / per_block, 256, 0, stream>>>(
         cu, seqs.kv_len_dev, seqs.page_table_dev, seqs.n_seqs, rows, per_block, seqs.table_stride, seqs.pages_per_seq, c.page_shift, c,
         k, k_stride, v, v_stride);
     ET_LAUNCH_CHECK();
     return ET_OK;
-  });
+  };
+  if (cache.format == ET_KV_MXFP4)
+    return kv_dispatch_mxfp4(cache.head_dim, [&](auto hd) { return launch(hd, std::integral_constant<int, ET_KV_MXFP4>()); });
+  return kv_dispatch(cache.head_dim, cache.format, launch);
 }
 
 }  // namespace et
@@ -301,8 +344,9 @@ extern "C" {
 size_t et_kv_page_bytes(int32_t page_size, int32_t n_kv_heads, int32_t head_dim, int32_t format) {
   const bool page_ok = page_size >= 16 && page_size <= 256 && (page_size & (page_size - 1)) == 0;
   const bool head_ok = head_dim == 64 || head_dim == 80 || head_dim == 96 || head_dim == 128 || head_dim == 256;
-  if (!page_ok || !head_ok || n_kv_heads < 1 || n_kv_heads > 1024 || format < ET_KV_BF16 || format > ET_KV_INT8) return 0;
-  const size_t row = format == ET_KV_BF16 ? 2 * (size_t)head_dim : (size_t)head_dim + 2;
+  if (!page_ok || !head_ok || n_kv_heads < 1 || n_kv_heads > 1024 || !kv_format(format)) return 0;
+  const size_t row = format == ET_KV_BF16 ? 2 * (size_t)head_dim : format == ET_KV_MXFP4 ? (size_t)(head_dim / 2 + kv_mx_blocks(head_dim))
+                                                                                          : (size_t)head_dim + 2;
   return 2 * row * (size_t)page_size * (size_t)n_kv_heads;
 }
 
