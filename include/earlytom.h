@@ -393,6 +393,11 @@ size_t et_kv_page_bytes(int32_t page_size, int32_t n_kv_heads, int32_t head_dim,
 int et_kv_append(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *cu_rows_dev, int32_t rows,
                  const uint16_t *k_dev, int64_t k_stride, const uint16_t *v_dev, int64_t v_stride, void *hip_stream);
 
+/* The same for rows whose places the caller has: row i goes to token slots_dev[i] % page_size of page slots_dev[i] / page_size;
+ * a negative slot, or one past the last page, is no place and its row is not stored.  (int64: et_kv_resize makes them.) */
+int et_kv_append_slots(const et_kv_cache *cache, const int64_t *slots_dev, int32_t rows, const uint16_t *k_dev, int64_t k_stride,
+                       const uint16_t *v_dev, int64_t v_stride, void *hip_stream);
+
 /* The inverse: the values that the cache's rows stand for, rounded to bf16 once.  Same rows, same strides, same errors. */
 int et_kv_read(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *cu_rows_dev, int32_t rows,
                uint16_t *k_out_dev, int64_t k_stride, uint16_t *v_out_dev, int64_t v_stride, void *hip_stream);
@@ -421,6 +426,75 @@ size_t et_attention_paged_workspace_bytes(const et_kv_cache *cache, const et_kv_
 int et_attention_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, const uint16_t *q_dev, int64_t q_stride,
                        int32_t n_heads, int32_t max_len, int32_t window, float scale, void *workspace_dev,
                        size_t workspace_bytes, uint16_t *out_dev, void *hip_stream);
+
+/* ---- pages for sequences that grow, shrink and end ------------------------------------------------
+ * The cache's free pages lie in a ring of n_pages cells; state = { first, free, missing, 0 }: `free` pages from cell `first` on.
+ * et_kv_resize takes every sequence b from kv_len[b] to new_len[b] tokens (negative lengths count as 0).  With pages(n) =
+ * min(ceil(n / page_size), pages_per_seq):
+ *   - entries pages(kv_len) .. pages(new_len) of its table row get pages from the ring's front, sequence by sequence and entry by entry;
+ *     once the ring is empty they get -1 (no page), and `missing` of the new state counts those;
+ *   - entries pages(new_len) .. pages(kv_len), of a sequence that shrinks or ends, give their pages back behind the ring's last one, in the same
+ *     order, to be taken from the next call on.  Entries that are no page give nothing, nor do pages for which the ring has no room.
+ * The new tokens of all sequences are consecutive rows, sequence by sequence: cu_rows [n_seqs + 1] their ranges (as et_kv_append takes
+ * them, with new_len as lengths), positions [rows] the place of each in its sequence, slots [rows] page * page_size + place in the page, or -1
+ * where there is no page (a missing one, or past pages_per_seq).  positions_dev and slots_dev may be NULL; `rows` is how many
+ * rows they have: rows past that are not written, nor is what lies behind the last sequence's.  cu_rows stops at 2^31 - 1.
+ * kv_len, new_len and everything else of the table stay as they are, and so do the ring's pages that were free: with another buffer as state_out_dev
+ * (state_out_dev = state_dev is allowed) a call is taken back by going on with the old state and the old lengths, as when
+ * pages are missing.  A page must be in one place, a table's live entry or a free cell of the ring; sequences that share pages are the
+ * caller's to keep apart.  Whatever state, ring, lengths and table hold, nothing outside them is touched.
+ * state_dev and state_out_dev int32 [4], aligned to 16 bytes; n_seqs at most 2^20, n_seqs * pages_per_seq below 2^31.  workspace:
+ * et_kv_resize_workspace_bytes (0 up to 1024 sequences and 8192 rows), aligned to 16 bytes, contents arbitrary.  Calls on the same ring,
+ * state or table follow each other in one stream.  Asynchronous on `hip_stream`; can be captured.  Errors: INVALID_ARG, WORKSPACE, HIP. */
+typedef struct {
+  int32_t *ring_dev;           /* [n_pages]                                                          */
+  int32_t n_pages, page_size;  /* page_size 16, 32, 64, 128 or 256                                   */
+} et_kv_pool;
+size_t et_kv_resize_workspace_bytes(int32_t n_seqs, int32_t rows);
+int et_kv_resize(const et_kv_pool *pool, const int32_t *state_dev, int32_t *state_out_dev, int32_t *page_table_dev,
+                 int32_t table_stride, int32_t pages_per_seq, const int32_t *kv_len_dev, const int32_t *new_len_dev,
+                 int32_t n_seqs, int32_t rows, int32_t *cu_rows_dev, int32_t *positions_dev, int64_t *slots_dev,
+                 void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/* ---- rotary positions of queries and keys ----------------------------------------------------------
+ * Pair i = 0 .. rot_dim / 2 - 1 of a head, dimensions (a, b) = (i, i + rot_dim / 2) (ET_ROTARY_HALF) or (2 i, 2 i + 1)
+ * (ET_ROTARY_INTERLEAVED), becomes  A (a cos t - b sin t, b cos t + a sin t),  t = position * f_i;  dimensions from rot_dim on stay
+ * as they are.  f_i = base^(-2 i / rot_dim), changed for contexts that are longer than those a model was trained with:
+ *   ET_ROTARY_LINEAR: f_i / factor.      ET_ROTARY_NTK: base * factor^(rot_dim / (rot_dim - 2)) in the place of base.
+ *   ET_ROTARY_YARN: f_i / factor * r + f_i * (1 - r), r rising from 0 to 1 between the pairs (whole numbers outwards) that turn `fast` and
+ *     `slow` times (32 and 1, usually) over original_len positions, i.e. i = rot_dim ln(original_len / (2 pi turns)) / (2 ln base);
+ *     A = 0.1 ln(factor) + 1.
+ *   ET_ROTARY_TURNS: the same mix, r falling from 1 to 0 as the number of turns original_len f_i / (2 pi) goes from `slow` to `fast` (1 and 4,
+ *     usually).
+ * A = 1 but for ET_ROTARY_YARN.  et_rotary_steps (host only) writes f_i as fractions of a turn, steps[i] = round(2^64 f_i / (2 pi)),
+ * [rot_dim / 2], and A; the caller puts the steps on the device.  position * steps[i] mod 2^64 is then the angle of any int32
+ * position, negative ones too, without loss.  base in [1, 1e30], factor in [1, 1e9]; scaling NULL: none.  Errors: INVALID_ARG. */
+enum { ET_ROTARY_HALF = 0, ET_ROTARY_INTERLEAVED = 1 };
+enum { ET_ROTARY_PLAIN = 0, ET_ROTARY_LINEAR = 1, ET_ROTARY_NTK = 2, ET_ROTARY_YARN = 3, ET_ROTARY_TURNS = 4 };
+typedef struct {
+  int32_t kind;
+  double factor, original_len, slow, fast; /* the last three: ET_ROTARY_YARN and ET_ROTARY_TURNS     */
+} et_rotary_scaling;
+int et_rotary_steps(const et_rotary_scaling *scaling, int32_t rot_dim, double base, uint64_t *steps, float *amplitude);
+
+typedef struct {
+  const uint64_t *steps_dev; /* [rot_dim / 2]                                                        */
+  int32_t head_dim, rot_dim, layout; /* even, rot_dim <= head_dim <= 512                             */
+  float amplitude;
+} et_rotary;
+typedef struct {
+  const uint16_t *in_dev; /* bf16 [rows, n_heads * head_dim], row stride in_stride (elements)        */
+  int64_t in_stride;
+  uint16_t *out_dev; /* may be in_dev, with the same stride; must not overlap it otherwise           */
+  int64_t out_stride;
+  int32_t n_heads;
+} et_rotary_rows;
+/* Turns rows of queries and (k NULL or n_heads 0: none) keys by positions_dev int32 [rows].  transpose = 1: by the transposed matrix, the
+ * way back where A = 1, and a gradient's way through.  Products and sums are float32, results rounded once; cosine and sine are within
+ * 2^-22 of A.  Any strides and alignments; 16 bytes and pairs in whole eighths (half: rot_dim a multiple of 16) are fastest.  rows at
+ * most 2^27 - 8.  Asynchronous on `hip_stream`.  Errors: INVALID_ARG, HIP. */
+int et_rotary_apply(const et_rotary *rotary, const int32_t *positions_dev, int32_t rows, const et_rotary_rows *q,
+                    const et_rotary_rows *k, int32_t transpose, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -65,6 +65,23 @@ class _KvSeqs(C.Structure):
                 ("kv_len_dev", C.c_void_p), ("n_seqs", C.c_int32)]
 
 
+class _KvPool(C.Structure):
+    _fields_ = [("ring_dev", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32)]
+
+
+class _RotaryScaling(C.Structure):
+    _fields_ = [("kind", C.c_int32)] + [(n, C.c_double) for n in ("factor", "original_len", "slow", "fast")]
+
+
+class _Rotary(C.Structure):
+    _fields_ = [("steps_dev", C.c_void_p)] + [(n, C.c_int32) for n in ("head_dim", "rot_dim", "layout")] + [("amplitude", C.c_float)]
+
+
+class _RotaryRows(C.Structure):
+    _fields_ = [("in_dev", C.c_void_p), ("in_stride", C.c_int64), ("out_dev", C.c_void_p), ("out_stride", C.c_int64),
+                ("n_heads", C.c_int32)]
+
+
 ET_MERGE_MEAN, ET_MERGE_ALG1 = 0, 1
 ET_SELECT_UNIFORM, ET_SELECT_DECOUPLED = 0, 1
 ET_SCORE_L2NORM, ET_SCORE_ATTENTION = 0, 1
@@ -122,6 +139,11 @@ def load_library():
         "et_project_tokens": (C.c_int, [vp, vp, i32, vp, sz, vp, vp]),
         "et_kv_page_bytes": (sz, [i32, i32, i32, i32]),
         "et_kv_append": (C.c_int, [C.POINTER(_KvCache), C.POINTER(_KvSeqs), vp, i32, vp, i64, vp, i64, vp]),
+        "et_kv_append_slots": (C.c_int, [C.POINTER(_KvCache), vp, i32, vp, i64, vp, i64, vp]),
+        "et_kv_resize_workspace_bytes": (sz, [i32, i32]),
+        "et_kv_resize": (C.c_int, [C.POINTER(_KvPool), vp, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]),
+        "et_rotary_steps": (C.c_int, [C.POINTER(_RotaryScaling), i32, C.c_double, C.POINTER(C.c_uint64), _FP]),
+        "et_rotary_apply": (C.c_int, [C.POINTER(_Rotary), vp, i32, C.POINTER(_RotaryRows), C.POINTER(_RotaryRows), i32, vp]),
         "et_kv_read": (C.c_int, [C.POINTER(_KvCache), C.POINTER(_KvSeqs), vp, i32, vp, i64, vp, i64, vp]),
         "et_attention_paged_workspace_bytes": (sz, [C.POINTER(_KvCache), C.POINTER(_KvSeqs), i32, i32, i32]),
         "et_attention_paged": (C.c_int, [C.POINTER(_KvCache), C.POINTER(_KvSeqs), vp, i64, i32, i32, i32, f32, vp, sz, vp, vp]),
@@ -577,7 +599,25 @@ def et_kv_page_bytes(page_size, n_kv_heads, head_dim, fmt):
     return int(load_library().et_kv_page_bytes(int(page_size), int(n_kv_heads), int(head_dim), _KV_FORMATS[fmt]))
 
 
-class KVCache:
+class _OnDevice:
+    """Something whose calls run on its own device (`device`), on that device's current stream or one that is given."""
+
+    def _here(self, stream):
+        """The stream to launch on, if its device is the current one and no other stream is asked for."""
+        if stream is None and _current_device() == self.device.index:
+            return _raw_stream(self.device.index)
+        return None
+
+    def _elsewhere(self, stream):
+        """Makes the device, and `stream` if given, current: allocations have to be made there too."""
+        if stream is None:
+            return torch.cuda.device(self.device)
+        if stream.device != self.device:
+            raise ValueError("the stream is on %s, not on %s" % (stream.device, self.device))
+        return torch.cuda.stream(stream)
+
+
+class KVCache(_OnDevice):
     """A paged key-value cache: `data` uint8 [n_pages, page bytes] on the device (layout in earlytom.h), allocated here unless
     given.  fmt: "bf16", "e4m3", "int8" or "mxfp4".  The sequences are the caller's: page_table int32 [n_seqs, pages] (entries outside
     [0, n_pages) = no page; rows may be strided), kv_len int32 [n_seqs].  Every call is asynchronous on `stream` (default: the
@@ -616,6 +656,23 @@ class KVCache:
         seqs = self._seqs(page_table, kv_len)
         _check(self._lib.et_kv_append(self._cache, seqs, None if cu_rows is None else self._cu(cu_rows, kv_len), rows, k.data_ptr(),
                                       k_stride, v.data_ptr(), v_stride, s))
+
+    def append_at(self, k, v, slots, stream=None):
+        """Stores rows as append does, at the places slots int64 [rows]: page * page_size + token of the page (negative or past the last
+        page: the row is not stored)."""
+        s = self._here(stream)
+        if s is None:
+            with self._elsewhere(stream):
+                return self.append_at(k, v, slots)
+        k, rows, _, k_stride = self._rows(k, "k", self._width)
+        v, v_rows, _, v_stride = self._rows(v, "v", self._width)
+        if v_rows != rows:
+            raise ValueError("k has %d rows, v %d" % (rows, v_rows))
+        if not (isinstance(slots, torch.Tensor) and slots.dtype is torch.int64 and slots.device == self.device):
+            raise TypeError("slots must be an int64 tensor on %s" % self.device)
+        if slots.shape != (rows,) or not slots.is_contiguous():
+            raise ValueError("slots must be contiguous, one for each of %d rows" % rows)
+        _check(self._lib.et_kv_append_slots(self._cache, slots.data_ptr(), rows, k.data_ptr(), k_stride, v.data_ptr(), v_stride, s))
 
     def read(self, page_table, kv_len, cu_rows=None, rows=None, out=None, stream=None):
         """The last cu_rows[b + 1] - cu_rows[b] tokens of every sequence b (None: one each) as bf16 rows (k, v), [rows,
@@ -701,19 +758,159 @@ class KVCache:
             raise ValueError("cu_rows must be contiguous, one more than there are sequences")
         return cu_rows.data_ptr()
 
-    def _here(self, stream):
-        """The stream to launch on, if its device is the current one and no other stream is asked for."""
-        if stream is None and _current_device() == self.device.index:
-            return _raw_stream(self.device.index)
-        return None
 
-    def _elsewhere(self, stream):
-        """Makes the cache's device, and `stream` if given, current: allocations have to be made there too."""
-        if stream is None:
-            return torch.cuda.device(self.device)
-        if stream.device != self.device:
-            raise ValueError("the stream is on %s, the cache on %s" % (stream.device, self.device))
-        return torch.cuda.stream(stream)
+class PagePool(_OnDevice):
+    """The free pages of a cache, for sequences that grow, shrink and end without the host: `ring` int32 [n_pages] and `state` int32 [4]
+    = first free cell, free pages, pages that were missing in the last call, 0 (all pages free unless given).  Calls are asynchronous
+    on `stream` as a KVCache's and can be captured; those on the same pool or table follow each other in one stream."""
+
+    def __init__(self, n_pages, page_size, ring=None, state=None, device="cuda:0"):
+        if n_pages < 1 or n_pages > _INT_MAX or page_size not in (16, 32, 64, 128, 256):
+            raise ValueError("no such pool: n_pages %d, page_size %d (16, 32, 64, 128, 256)" % (n_pages, page_size))
+        if ring is None:
+            ring = torch.arange(n_pages, dtype=torch.int32, device=device)
+        if state is None:
+            state = torch.tensor([0, n_pages, 0, 0], dtype=torch.int32, device=ring.device)
+        _dev(ring, torch.int32, "ring")
+        _dev(state, torch.int32, "state")
+        if ring.shape != (n_pages,) or state.shape != (4,) or state.device != ring.device:
+            raise ValueError("ring must have n_pages = %d values, state 4, on one device" % n_pages)
+        self.ring, self.state, self.device = ring, state, ring.device
+        self.n_pages, self.page_size, self._lib = int(n_pages), int(page_size), load_library()
+        self._pool = _KvPool(ring.data_ptr(), self.n_pages, self.page_size)
+
+    def resize(self, page_table, kv_len, new_len, rows, state_out=None, out=None, stream=None):
+        """Takes every sequence from kv_len to new_len tokens (int32 [n_seqs] each): its row of page_table (int32 [n_seqs, pages], rows may
+        be strided) gets pages from the pool, or gives back those that it no longer needs.  Returns (cu_rows int32 [n_seqs + 1], positions
+        int32 [rows], slots int64 [rows]) of the new tokens, sequence by sequence; `rows` is how many there are, as the caller knows, or a bound
+        (rows behind the last sequence's hold anything, or stay as `out`, the same three, has them).  The pool's state is changed in
+        place, or goes to state_out int32 [4]: then the call is taken back by going on with the old state and lengths."""
+        s = self._here(stream)
+        if s is None:
+            with self._elsewhere(stream):
+                return self.resize(page_table, kv_len, new_len, rows, state_out, out)
+        shape, strides = self._ints(page_table, "page_table").shape, page_table.stride()
+        if len(shape) != 2 or shape[1] < 1 or (strides[1] != 1 and shape[1] > 1):
+            raise ValueError("page_table must be [n_seqs, pages] with contiguous rows")
+        n, pages = shape
+        for t, name in ((kv_len, "kv_len"), (new_len, "new_len")):
+            if self._ints(t, name).shape != (n,) or not t.is_contiguous():
+                raise ValueError("%s must be contiguous, one for each row of page_table" % name)
+        if state_out is None:
+            state_out = self.state
+        elif self._ints(state_out, "state_out").shape != (4,) or not state_out.is_contiguous():
+            raise ValueError("state_out must be contiguous, of 4 values")
+        rows = int(rows)
+        if rows < 0 or rows > _INT_MAX:
+            raise ValueError("rows = %d must be in [0, 2^31 - 1]" % rows)
+        if out is None:
+            cu = torch.empty(n + 1, dtype=torch.int32, device=self.device)
+            out = cu, torch.empty(rows, dtype=torch.int32, device=self.device), torch.empty(rows, dtype=torch.int64, device=self.device)
+        else:
+            if not all(t.is_contiguous() and t.device == self.device for t in out) or \
+                    [t.dtype for t in out] != [torch.int32, torch.int32, torch.int64] or \
+                    out[0].shape != (n + 1,) or out[1].numel() < rows or out[2].numel() < rows:
+                raise ValueError("out must be cu_rows int32 [%d], positions int32 and slots int64 [%d], contiguous, on %s" % (n + 1, rows, self.device))
+        need = self._lib.et_kv_resize_workspace_bytes(n, rows)
+        ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        cu, positions, slots = out
+        _check(self._lib.et_kv_resize(self._pool, self.state.data_ptr(), state_out.data_ptr(), page_table.data_ptr(), strides[0] if n > 1 else pages,
+                                      pages, kv_len.data_ptr(), new_len.data_ptr(), n, rows, cu.data_ptr(), positions.data_ptr(),
+                                      slots.data_ptr(), ws.data_ptr() if need else None, need, s))
+        return out
+
+    def _ints(self, t, name):
+        if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.device == self.device):
+            raise TypeError("%s must be an int32 tensor on %s" % (name, self.device))
+        return t
+
+
+_ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+_ROTARY_SCALINGS = {"linear": 1, "ntk": 2, "yarn": 3, "turns": 4}
+_ROTARY_TURNS = {"yarn": (1.0, 32.0), "turns": (1.0, 4.0)}
+
+
+def et_rotary_steps(rot_dim, base=10000.0, scaling=None):
+    """(uint64 [rot_dim / 2]: every pair's turn per position, in units of 2^-64; the factor A).  scaling: None or a dict with `kind` ("linear",
+    "ntk", "yarn", "turns"), `factor`, and for the last two `original_len` and, if wanted, `slow` and `fast`."""
+    sc = None
+    if scaling is not None:
+        left = dict(scaling)
+        kind = left.pop("kind")
+        if kind not in _ROTARY_SCALINGS:
+            raise ValueError("kind must be one of %s" % ", ".join(_ROTARY_SCALINGS))
+        slow, fast = _ROTARY_TURNS.get(kind, (0.0, 0.0))
+        values = [float(left.pop("factor"))]
+        if kind in _ROTARY_TURNS:
+            values += [float(left.pop("original_len")), float(left.pop("slow", slow)), float(left.pop("fast", fast))]
+        if left:
+            raise ValueError("%s does not take %s" % (kind, ", ".join(sorted(left))))
+        sc = _RotaryScaling(_ROTARY_SCALINGS[kind], *values)
+    steps, amplitude = np.zeros(max(int(rot_dim) // 2, 1), dtype=np.uint64), C.c_float()
+    _check(load_library().et_rotary_steps(None if sc is None else C.byref(sc), int(rot_dim), float(base),
+                                          steps.ctypes.data_as(C.POINTER(C.c_uint64)), C.byref(amplitude)))
+    return steps, float(amplitude.value)
+
+
+class Rotary(_OnDevice):
+    """Rotary positions for heads of head_dim, whose first rot_dim dimensions turn (default: all).  layout: "half" (pairs i and i +
+    rot_dim / 2) or "interleaved" (2 i and 2 i + 1); scaling as et_rotary_steps takes it; amplitude: instead of the scaling's factor A.  The
+    steps go to the device once, here; calls are asynchronous on `stream` as a KVCache's and can be captured."""
+
+    def __init__(self, head_dim, rot_dim=None, base=10000.0, layout="half", scaling=None, amplitude=None, device="cuda:0"):
+        rot_dim = head_dim if rot_dim is None else rot_dim
+        if layout not in _ROTARY_LAYOUTS:
+            raise ValueError("layout must be one of %s" % ", ".join(_ROTARY_LAYOUTS))
+        if not (2 <= head_dim <= 512 and head_dim % 2 == 0 and 2 <= rot_dim <= head_dim and rot_dim % 2 == 0):
+            raise ValueError("no such heads: head_dim %d and rot_dim %d must be even, 2 <= rot_dim <= head_dim <= 512" % (head_dim, rot_dim))
+        steps, factor = et_rotary_steps(rot_dim, base, scaling)
+        self.head_dim, self.rot_dim, self.amplitude = int(head_dim), int(rot_dim), factor if amplitude is None else float(amplitude)
+        self.steps = torch.from_numpy(steps.view(np.int64)).to(device)
+        self.device, self._lib = self.steps.device, load_library()
+        self._rotary = _Rotary(self.steps.data_ptr(), self.head_dim, self.rot_dim, _ROTARY_LAYOUTS[layout], self.amplitude)
+
+    def apply(self, q, k, positions, out=None, transpose=False, stream=None):
+        """Turns q and k, bf16 [rows, heads * head_dim] or [rows, heads, head_dim] (rows may be strided; k may be None), by positions int32
+        [rows]; returns both, contiguous, or in `out` = (q, k), which may be q and k themselves.  transpose: by the transposed matrix (the way
+        back, and a gradient's)."""
+        s = self._here(stream)
+        if s is None:
+            with self._elsewhere(stream):
+                return self.apply(q, k, positions, out, transpose)
+        if not (isinstance(positions, torch.Tensor) and positions.dtype is torch.int32 and positions.device == self.device):
+            raise TypeError("positions must be an int32 tensor on %s" % self.device)
+        rows = positions.shape[0] if positions.dim() == 1 else -1
+        if rows < 0 or not positions.is_contiguous():
+            raise ValueError("positions must be contiguous, one for each row")
+        out = (None, None) if out is None else out
+        q_out, q_rows = self._turned(q, out[0], "q", rows)
+        k_out, k_rows = (None, None) if k is None else self._turned(k, out[1], "k", rows)
+        _check(self._lib.et_rotary_apply(self._rotary, positions.data_ptr(), rows, q_rows, k_rows, int(bool(transpose)), s))
+        return q_out, k_out
+
+    def _turned(self, x, out, name, rows):
+        ptr, heads, stride = self._heads(x, name, rows)
+        if out is None:
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+            return out, _RotaryRows(ptr, stride, out.data_ptr(), heads * self.head_dim, heads)
+        to, to_heads, to_stride = self._heads(out, "out of " + name, rows)
+        if to_heads != heads:
+            raise ValueError("%s has %d heads, its out %d" % (name, heads, to_heads))
+        return out, _RotaryRows(ptr, stride, to, to_stride, heads)
+
+    def _heads(self, t, name, rows):
+        if not (isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.device == self.device):
+            raise TypeError("%s must be a bfloat16 tensor on %s" % (name, self.device))
+        shape, strides, d = t.shape, t.stride(), self.head_dim
+        if len(shape) == 3 and shape[2] == d and strides[2] == 1 and (strides[1] == d or shape[1] == 1):
+            heads = shape[1]
+        elif len(shape) == 2 and strides[1] == 1 and shape[1] % d == 0:
+            heads = shape[1] // d
+        else:
+            raise ValueError("%s must be [rows, heads * %d] or [rows, heads, %d] with contiguous rows" % (name, d, d))
+        if shape[0] != rows:
+            raise ValueError("%s has %d rows for %d positions" % (name, shape[0], rows))
+        return t.data_ptr(), heads, strides[0] if rows > 1 else heads * d
 
 
 class Encoder:

@@ -64,6 +64,21 @@ __device__ __forceinline__ KvPlace kv_place(const int32_t *cu, int first, int co
   return out;
 }
 
+// The same where the caller knows the rows' places.
+__device__ __forceinline__ KvPlace kv_slot(const int64_t *slots, int first, int count, int n_pages, int page_shift) {
+  KvPlace out{0, -1, 0};
+  const int lane = threadIdx.x & 63;
+  if (lane < count) {
+    const int64_t slot = slots[first + lane];
+    out.owned = 1;
+    if (slot >= 0 && slot >> page_shift < n_pages) {
+      out.page = (int)(slot >> page_shift);
+      out.at = (int)slot & ((1 << page_shift) - 1);
+    }
+  }
+  return out;
+}
+
 // Lanes that share a head's row, eight values each; those past the row's end idle.
 template <int HD>
 constexpr int kv_lanes() { return HD <= 64 ? 8 : HD <= 128 ? 16 : 32; }
@@ -180,13 +195,15 @@ constexpr int kBatch = 4;
 template <int HD, int FMT, bool STORE>
 __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const int32_t *len, const int32_t *table, int n_seqs, int rows,
                                                       int per_block, int table_stride, int pages_per_seq, int page_shift, KvPages c,
-                                                      uint16_t *k, int64_t k_stride, uint16_t *v, int64_t v_stride) {
+                                                      uint16_t *k, int64_t k_stride, uint16_t *v, int64_t v_stride,
+                                                      const int64_t *slots) {
   using Lay = KvLayout<HD, FMT>;
   constexpr int LANES = kv_lanes<HD>(), GROUPS = 256 / LANES;
   __shared__ int4 lds_place[64];                         // byte offset of the page (two words), token of the page, 0 / 1 / 2
   const int first = blockIdx.x * per_block, count = min(per_block, rows - first);
   if (threadIdx.x < 64) {
-    const KvPlace p = kv_place(cu, first, count, KvSeqs{table, len, table_stride, pages_per_seq, n_seqs}, c.n_pages, page_shift);
+    const KvPlace p = slots ? kv_slot(slots, first, count, c.n_pages, page_shift)
+                            : kv_place(cu, first, count, KvSeqs{table, len, table_stride, pages_per_seq, n_seqs}, c.n_pages, page_shift);
     const int64_t page = max(p.page, 0) * c.page_bytes;
     lds_place[threadIdx.x] = make_int4((int)page, (int)(page >> 32), p.at, p.owned ? (p.page >= 0 ? 2 : 1) : 0);
   }
@@ -267,9 +284,8 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const i
 
 static bool kv_format(int format) { return (format >= ET_KV_BF16 && format <= ET_KV_INT8) || format == ET_KV_MXFP4; }
 
-int check_kv(const et_kv_cache *c, const et_kv_seqs *s) {
+static int check_cache(const et_kv_cache *c) {
   ET_REQUIRE(c != nullptr, "cache is NULL");
-  ET_REQUIRE(s != nullptr, "seqs is NULL");
   ET_REQUIRE(kv_format(c->format), "unknown cache format %d", c->format);
   ET_REQUIRE(c->n_kv_heads >= 1 && c->n_kv_heads <= 1024, "n_kv_heads = %d must be in [1, 1024]", c->n_kv_heads);
   ET_REQUIRE(c->n_pages >= 1, "n_pages = %d must be at least 1", c->n_pages);
@@ -279,6 +295,13 @@ int check_kv(const et_kv_cache *c, const et_kv_seqs *s) {
     return ET_ERR_UNSUPPORTED;
   }
   ET_REQUIRE(c->data_dev != nullptr && (uintptr_t)c->data_dev % 16 == 0, "data_dev of the cache is NULL or not aligned to 16 bytes");
+  return ET_OK;
+}
+int check_kv(const et_kv_cache *c, const et_kv_seqs *s) {
+  ET_REQUIRE(c != nullptr, "cache is NULL");
+  ET_REQUIRE(s != nullptr, "seqs is NULL");
+  int rc;
+  if ((rc = check_cache(c))) return rc;
   ET_REQUIRE(s->n_seqs >= 0, "n_seqs = %d is negative", s->n_seqs);
   ET_REQUIRE(s->pages_per_seq >= 1 && s->table_stride >= s->pages_per_seq && (int64_t)s->pages_per_seq * c->page_size <= 1 << 30,
              "pages_per_seq = %d must be at least 1, at most table_stride = %d, and at most 2^30 tokens", s->pages_per_seq, s->table_stride);
@@ -292,17 +315,20 @@ KvPages kv_pages(const et_kv_cache &c) {
 }
 // A launch takes fewer than 2^32 lanes, 256 a workgroup, and a workgroup at most 64 rows.
 constexpr int kMaxBlocks = (1 << 24) - 1, kMaxRows = 64 * kMaxBlocks;
-static int check_rows(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *cu, int rows, const void *k, int64_t k_stride,
-                      const void *v, int64_t v_stride) {
-  int rc;
-  if ((rc = check_kv(cache, seqs))) return rc;
+static int check_row_data(const et_kv_cache *cache, int rows, const void *k, int64_t k_stride, const void *v, int64_t v_stride) {
   ET_REQUIRE(rows >= 0 && rows <= kMaxRows, "rows = %d must be in [0, 2^30 - 64]", rows);
-  ET_REQUIRE(cu || rows == seqs->n_seqs, "rows = %d without cu_rows_dev must be n_seqs = %d", rows, seqs->n_seqs);
   if (rows == 0) return ET_OK;
   const int64_t width = (int64_t)cache->n_kv_heads * cache->head_dim;
   ET_REQUIRE(k && v && (uintptr_t)k % 16 == 0 && (uintptr_t)v % 16 == 0, "a key or value pointer is NULL or not aligned to 16 bytes");
   ET_REQUIRE(k_stride >= width && v_stride >= width && k_stride % 8 == 0 && v_stride % 8 == 0,
              "row strides %lld and %lld must be multiples of 8 and at least %lld", (long long)k_stride, (long long)v_stride, (long long)width);
+  return ET_OK;
+}
+static int check_rows(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *cu, int rows, const void *k, int64_t k_stride,
+                      const void *v, int64_t v_stride) {
+  int rc;
+  if ((rc = check_kv(cache, seqs)) || (rc = check_row_data(cache, rows, k, k_stride, v, v_stride))) return rc;
+  ET_REQUIRE(cu || rows == seqs->n_seqs, "rows = %d without cu_rows_dev must be n_seqs = %d", rows, seqs->n_seqs);
   return ET_OK;
 }
 
@@ -318,15 +344,15 @@ static int rows_per_block(int rows, const et_kv_cache &c) {
 }
 
 template <bool STORE>
-static int launch_rows(const et_kv_cache &cache, const et_kv_seqs &seqs, const int32_t *cu, int rows, uint16_t *k, int64_t k_stride,
-                       uint16_t *v, int64_t v_stride, hipStream_t stream) {
-  if (rows == 0 || seqs.n_seqs == 0) return ET_OK;
+static int launch_rows(const et_kv_cache &cache, const et_kv_seqs &seqs, const int32_t *cu, const int64_t *slots, int rows, uint16_t *k,
+                       int64_t k_stride, uint16_t *v, int64_t v_stride, hipStream_t stream) {
+  if (rows == 0 || (seqs.n_seqs == 0 && !slots)) return ET_OK;
   const KvPages c = kv_pages(cache);
   const int per_block = rows_per_block(rows, cache);
   auto launch = [&](auto hd, auto fmt) {
     kv_rows_kernel<hd.value, fmt.value, STORE><<<(rows + per_block - 1) / per_block, 256, 0, stream>>>(
         cu, seqs.kv_len_dev, seqs.page_table_dev, seqs.n_seqs, rows, per_block, seqs.table_stride, seqs.pages_per_seq, c.page_shift, c,
-        k, k_stride, v, v_stride);
+        k, k_stride, v, v_stride, slots);
     ET_LAUNCH_CHECK();
     return ET_OK;
   };
@@ -354,7 +380,16 @@ int et_kv_append(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t
                  int64_t k_stride, const uint16_t *v_dev, int64_t v_stride, void *hip_stream) {
   int rc;
   if ((rc = check_rows(cache, seqs, cu_rows_dev, rows, k_dev, k_stride, v_dev, v_stride))) return rc;
-  return launch_rows<true>(*cache, *seqs, cu_rows_dev, rows, const_cast<uint16_t *>(k_dev), k_stride, const_cast<uint16_t *>(v_dev),
+  return launch_rows<true>(*cache, *seqs, cu_rows_dev, nullptr, rows, const_cast<uint16_t *>(k_dev), k_stride, const_cast<uint16_t *>(v_dev),
+                           v_stride, static_cast<hipStream_t>(hip_stream));
+}
+
+int et_kv_append_slots(const et_kv_cache *cache, const int64_t *slots_dev, int32_t rows, const uint16_t *k_dev, int64_t k_stride,
+                       const uint16_t *v_dev, int64_t v_stride, void *hip_stream) {
+  int rc;
+  if ((rc = check_cache(cache)) || (rc = check_row_data(cache, rows, k_dev, k_stride, v_dev, v_stride))) return rc;
+  ET_REQUIRE(rows == 0 || (slots_dev && (uintptr_t)slots_dev % 8 == 0), "slots_dev is NULL or not aligned to 8 bytes");
+  return launch_rows<true>(*cache, et_kv_seqs{}, nullptr, slots_dev, rows, const_cast<uint16_t *>(k_dev), k_stride, const_cast<uint16_t *>(v_dev),
                            v_stride, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -362,7 +397,7 @@ int et_kv_read(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *
                int64_t k_stride, uint16_t *v_out_dev, int64_t v_stride, void *hip_stream) {
   int rc;
   if ((rc = check_rows(cache, seqs, cu_rows_dev, rows, k_out_dev, k_stride, v_out_dev, v_stride))) return rc;
-  return launch_rows<false>(*cache, *seqs, cu_rows_dev, rows, k_out_dev, k_stride, v_out_dev, v_stride,
+  return launch_rows<false>(*cache, *seqs, cu_rows_dev, nullptr, rows, k_out_dev, k_stride, v_out_dev, v_stride,
                             static_cast<hipStream_t>(hip_stream));
 }
 
