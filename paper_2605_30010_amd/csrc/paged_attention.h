@@ -106,7 +106,7 @@ __device__ __forceinline__ float part_factor(float2 ml, float top) {
 }
 // What the values' codes are multiplied with at the end (their rows' maxima went into the weights, times 2^-9).
 template <int FMT>
-__device__ __forceinline__ float value_factor() { return FMT == ET_KV_BF16 || FMT == ET_KV_MXFP4 ? 1.f : 1.f / (kv_qmax<FMT>() * 0x1p-9f); }
+__device__ __forceinline__ float value_factor() { return FMT == ET_KV_BF16 ? 1.f : 1.f / (kv_qmax<FMT>() * 0x1p-9f); }
 
 // bf16 pair of two 8-bit codes, bytes 2 SEL and 2 SEL + 1 of w; exact in both formats.
 template <int FMT, int SEL>
@@ -127,7 +127,6 @@ template <int HD, int FMT>
 struct Keys {
   static constexpr int STEPS = (HD + 31) / 32, kRow = KvLayout<HD, FMT>::kRow;
   static constexpr bool WIDE = FMT == ET_KV_BF16;
-  static constexpr int UNITS = 1;                         // (4 bits only)
   static constexpr int PAIRS = WIDE ? 0 : STEPS / 2, NREG = WIDE ? STEPS * 4 : PAIRS * 4 + (STEPS % 2) * 2;
   static __device__ __forceinline__ int dim(int s, int g) {
     return WIDE || s >= 2 * PAIRS ? s * 32 + g * 8 : (s / 2) * 64 + g * 16 + (s % 2) * 8;
@@ -204,73 +203,6 @@ struct Values {
   }
 };
 
-// Keys in 4 bits.  A lane's load serves several steps of 32 dimensions, and so does its exponent: where a row is a multiple of 128,
-// 32 dimensions (a block) for four steps, elsewhere 16 (half a block) for two, and the third step has the dimensions from 64 on.
-template <int HD>
-struct Keys<HD, ET_KV_MXFP4> {
-  using Lay = KvLayout<HD, ET_KV_MXFP4>;
-  static constexpr int STEPS = (HD + 31) / 32, NREG = STEPS;
-  static constexpr bool WIDE = HD % 128 == 0;
-  static constexpr int UNITS = WIDE ? STEPS / 4 : STEPS - 1;             // exponents of a lane
-  static __device__ __forceinline__ int dim(int s, int g) {
-    return WIDE ? s / 4 * 128 + g * 32 + s % 4 * 8 : s < 2 ? g * 16 + s * 8 : 64 + g * 8;
-  }
-  // Past the row's end the last dimensions are read again (and not used).
-  static __device__ __forceinline__ void load(const char *base, int r, int g, uint32_t (&w)[NREG]) {
-    if constexpr (WIDE) {
-#pragma unroll
-      for (int i = 0; i < STEPS / 4; ++i) {
-        const u32x4 v = *reinterpret_cast<const u32x4 *>(base + (uint32_t)(r * Lay::kRow + i * 64 + g * 16));
-        w[4 * i] = v[0], w[4 * i + 1] = v[1], w[4 * i + 2] = v[2], w[4 * i + 3] = v[3];
-      }
-    } else {
-      const uint2 v = *reinterpret_cast<const uint2 *>(base + (uint32_t)(r * Lay::kRow + g * 8));
-      w[0] = v.x, w[1] = v.y;
-      if constexpr (STEPS > 2) w[2] = *reinterpret_cast<const uint32_t *>(base + (uint32_t)(r * Lay::kRow + min(32 + g * 4, Lay::kRow - 4)));
-    }
-  }
-  static __device__ __forceinline__ void load_units(const char *exponents, int r, int g, uint32_t (&u)[UNITS]) {
-    const uint8_t *e = reinterpret_cast<const uint8_t *>(exponents) + (uint32_t)(r * Lay::kBlocks);
-    if constexpr (WIDE) {
-#pragma unroll
-      for (int i = 0; i < UNITS; ++i) u[i] = (uint32_t)e[4 * i + g];
-    } else {
-      u[0] = (uint32_t)e[g / 2];
-      if constexpr (STEPS > 2) u[1] = (uint32_t)e[2];
-    }
-  }
-  static __device__ __forceinline__ u32x4 operand(const uint32_t (&w)[NREG], const uint32_t (&u)[UNITS], int s, int g) {
-    const u32x4 v = mx_decode8(w[s], u[WIDE ? s / 4 : s / 2]);
-    return HD % 32 && s == STEPS - 1 && 64 + g * 8 >= HD ? u32x4{0, 0, 0, 0} : v;
-  }
-};
-// Values in 4 bits: a lane's dimensions of a token are one load of 2 or 4 bytes, become bfloat16 pairs with the exponent of their block,
-// and go on as bfloat16 values do.
-template <int HD>
-struct Values<HD, ET_KV_MXFP4> {
-  using Lay = KvLayout<HD, ET_KV_MXFP4>;
-  using Wide = Values<HD, ET_KV_BF16>;
-  static constexpr int DPL = Wide::DPL, BLOCKS = Wide::BLOCKS, NREG = Wide::NREG;
-  // the codes of the lane's dimensions
-  static __device__ __forceinline__ uint32_t load(const char *base, int token, int r, int blk) {
-    const char *at = base + (uint32_t)(token * Lay::kRow + (blk * 128 + min(r, HD / DPL - 1) * DPL) / 2);
-    if constexpr (DPL == 8) return *reinterpret_cast<const uint32_t *>(at);
-    else return *reinterpret_cast<const uint16_t *>(at);
-  }
-  // the exponents of four tokens from `token` on, a byte each
-  static __device__ __forceinline__ uint32_t load_units(const char *exponents, int page_size, int token, int r, int blk) {
-    const int block = blk * 4 + min(r, HD / DPL - 1) * DPL / kMxBlock;
-    return *reinterpret_cast<const uint32_t *>(exponents + (uint32_t)(block * page_size + token));
-  }
-  // token e of those four (its exponent moves to where float32 has it; what comes along does not count)
-  static __device__ __forceinline__ void widen(uint32_t code, uint32_t units, int e, uint32_t (&w)[NREG]) {
-    const uint32_t unit = e == 0 ? units << 23 : e == 1 ? units << 15 : e == 2 ? units << 7 : units >> 1;
-    w[0] = mx_pair<0>(code, unit), w[1] = mx_pair<1>(code, unit);
-    if constexpr (DPL == 8) w[2] = mx_pair<2>(code, unit), w[3] = mx_pair<3>(code, unit);
-  }
-  static __device__ __forceinline__ u32x4 operand(const uint32_t (&w)[8][NREG], int j) { return Wide::operand(w, j); }
-};
-
 struct PagedMore {                                       // the kernel's arguments that its first loads do not need
   const uint16_t *q;
   int64_t q_stride;
@@ -282,6 +214,65 @@ struct PagedMore {                                       // the kernel's argumen
   int n_pages;
   float scale_log2;
 };
+// The end of a workgroup's part: its wavefronts' results (accumulators, reference m and this lane's sum of query head r) together, and out,
+// or to where the parts are joined.  `factor`: what the values are multiplied with.
+template <int HD, int DPL, int BLOCKS>
+__device__ __forceinline__ void finish_part(const PagedMore &o, const Part &part, const f32x4 (&acc)[BLOCKS * DPL], float m, float sum, float factor,
+                                            int wave, int live, int64_t head, int64_t slot, float (&lds_o)[kWaves][HD / BLOCKS][16],
+                                            float2 (&lds_ml)[kWaves][16]) {
+  constexpr int BD = HD / BLOCKS;                         // dimensions that the wavefronts add up at a time
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, h = threadIdx.x & 15;
+  sum += __shfl_xor(sum, 16, 64);
+  sum += __shfl_xor(sum, 32, 64);
+  if (g == 0) lds_ml[wave][r] = make_float2(m, sum);
+  float top = -INFINITY, total = 0.f, f[kWaves];
+#pragma unroll
+  for (int blk = 0; blk < BLOCKS; ++blk) {
+    if (blk) __syncthreads();
+    if (r < live) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int d = (4 * g + e) * DPL;
+        if (d < BD)
+#pragma unroll
+          for (int j = 0; j < DPL; ++j) lds_o[wave][d + j][r] = acc[blk * DPL + j][e];
+      }
+    }
+    __syncthreads();
+    if (blk == 0) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds_ml[w][h].x);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float2 ml = lds_ml[w][h];
+        f[w] = part_factor(ml, top);
+        total += f[w] * ml.y;
+      }
+    }
+    for (int d = (threadIdx.x >> 4) * 8; h < live && d < BD; d += 4 * kWaves * 8) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) x[e] = fmaf(f[w], lds_o[w][d + e][h], x[e]);
+      }
+      if (part.count == 1) {
+        const float inv = factor / total;
+        u32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = total == 0.f ? 0 : cvt_pk_bf16(x[2 * e] * inv, x[2 * e + 1] * inv);  // (0 times x could be NaN)
+        *reinterpret_cast<u32x4 *>(o.out + head * HD + blk * BD + d) = v;
+      } else {
+        float *to = o.part_o + slot * HD + blk * BD + d;
+        *reinterpret_cast<f32x4 *>(to) = f32x4{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<f32x4 *>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
+      }
+    }
+  }
+  if (part.count > 1 && threadIdx.x < live) o.part_ml[slot] = make_float2(top, total);
+}
+
 // A workgroup takes one part of a sequence's tokens for up to 16 query heads of one key-value head; its wavefronts take tiles of
 // 32 tokens in turn: logits S^T = K Q^T, weights against a running reference, O^T += V^T P^T, where the accumulators that hold S^T are,
 // exponentiated and rounded, operand B of the second product (which tokens a lane's eight places of the contraction stand for is free, and the
@@ -302,8 +293,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
   using K = Keys<HD, FMT>;
   using V = Values<HD, FMT>;
   constexpr int ACC = V::BLOCKS * V::DPL;
-  constexpr bool kMx = FMT == ET_KV_MXFP4;
-  constexpr bool kAhead = kMx || HD <= 128;               // a tile's keys are fetched during the one before: heads of 256 have no registers for it
+  constexpr bool kAhead = HD <= 128;                      // a tile's keys are fetched during the one before: heads of 256 have no registers for it
   constexpr int BD = HD / V::BLOCKS;                      // dimensions that the wavefronts add up at a time
   __shared__ float lds_o[kWaves][BD][16];
   __shared__ float2 lds_ml[kWaves][16];
@@ -349,8 +339,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
   auto head_of = [&](int page) { return o.data + max(page, 0) * o.page_bytes + (int64_t)kv * Lay::head_bytes(ps); };
   struct Tile {
     uint32_t kw[2][K::NREG];
-    std::conditional_t<kMx, uint32_t[2][K::UNITS], uint2[2]> km;          // what scales the keys
-    uint2 vm[2];                                          // and the values
+    uint2 km[2], vm[2];
     int page[2];
   };
   auto load_keys = [&](Tile &x, int t, int i) {
@@ -360,8 +349,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
       const int at = (start + t * kTile + 16 * u) & (ps - 1);
       const char *head = head_of(x.page[u]);
       K::load(head + at * Lay::kRow, r, g, x.kw[u]);
-      if constexpr (kMx) K::load_units(head + Lay::key_scale(ps) + at * Lay::kBlocks, r, g, x.km[u]);
-      else if constexpr (FMT != ET_KV_BF16) {
+      if constexpr (FMT != ET_KV_BF16) {
         x.km[u] = *reinterpret_cast<const uint2 *>(head + Lay::key_scale(ps) + (at + 4 * g) * 2);
         x.vm[u] = *reinterpret_cast<const uint2 *>(head + Lay::value_scale(ps) + (at + 4 * g) * 2);
       }
@@ -382,24 +370,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
     if (!kAhead && t != wave) load_keys(next, t, i);
     const Tile cur = next;
     const int pos0 = start + t * kTile;
-    const auto &km = cur.km;
-    const auto &vm = cur.vm;
+    const uint2 *km = cur.km, *vm = cur.vm;
     const int *page = cur.page;
     const auto &kw = cur.kw;
-    uint32_t vw[8][V::NREG], code[8], unit[2];
+    uint32_t vw[8][V::NREG];
     auto load_values = [&](int blk) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int at = (pos0 + 16 * u) & (ps - 1);
-        const char *head = head_of(page[u]), *values = head + Lay::values(ps) + at * Lay::kRow;
-        if constexpr (kMx) {
+        const char *values = head_of(page[u]) + Lay::values(ps) + ((pos0 + 16 * u) & (ps - 1)) * Lay::kRow;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) code[4 * u + e] = V::load(values, 4 * g + e, r, blk);
-          unit[u] = V::load_units(head + Lay::value_scale(ps), ps, at + 4 * g, r, blk);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) V::load(values, 4 * g + e, r, blk, vw[4 * u + e]);
-        }
+        for (int e = 0; e < 4; ++e) V::load(values, 4 * g + e, r, blk, vw[4 * u + e]);
       }
     };
     load_values(0);
@@ -410,14 +390,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
     for (int u = 0; u < 2; ++u) {
       f32x4 d{0, 0, 0, 0};
 #pragma unroll
-      for (int st = 0; st < K::STEPS; ++st) {
-        if constexpr (kMx) d = mfma16(K::operand(kw[u], km[u], st, g), qf[st], d);
-        else d = mfma16(K::operand(kw[u], st, g), qf[st], d);
-      }
+      for (int st = 0; st < K::STEPS; ++st) d = mfma16(K::operand(kw[u], st, g), qf[st], d);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float f = o.scale_log2;
-        if constexpr (FMT != ET_KV_BF16 && !kMx) f *= e & 1 ? bf16hi_to_f32(e & 2 ? km[u].y : km[u].x) : bf16lo_to_f32(e & 2 ? km[u].y : km[u].x);
+        if constexpr (FMT != ET_KV_BF16) f *= e & 1 ? bf16hi_to_f32(e & 2 ? km[u].y : km[u].x) : bf16lo_to_f32(e & 2 ? km[u].y : km[u].x);
         z[4 * u + e] = whole_product(d[e], f);
       }
     }
@@ -452,7 +429,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
     for (int e = 0; e < 8; ++e) {
       p[e] = __builtin_amdgcn_exp2f(z[e] - ref);
       sum += p[e];
-      if constexpr (FMT != ET_KV_BF16 && !kMx) {
+      if constexpr (FMT != ET_KV_BF16) {
         const uint32_t w = e & 2 ? vm[e / 4].y : vm[e / 4].x;
         p[e] *= (e & 1 ? bf16hi_to_f32(w) : bf16lo_to_f32(w)) * 0x1p-9f;
         if (!whole && (dead >> e & 1)) p[e] = 0.f;
@@ -469,10 +446,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
     }
 #pragma unroll
     for (int blk = 0; blk < V::BLOCKS; ++blk) {
-      if constexpr (kMx) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) V::widen(code[e], unit[e / 4], e & 3, vw[e]);
-      }
       if (!whole) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -490,58 +463,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
   }
 
   // the wavefronts' results together
-  sum += __shfl_xor(sum, 16, 64);
-  sum += __shfl_xor(sum, 32, 64);
-  if (g == 0) lds_ml[wave][r] = make_float2(m, sum);
   const int h = threadIdx.x & 15;
   const int64_t head = (int64_t)b * n_heads + (int64_t)kv * group + rt * 16 + h;
   const int64_t slot = (int64_t)item * n_heads + kv * group + rt * 16 + h;       // of a part that is one of several
-  float top = -INFINITY, total = 0.f, f[kWaves];
-#pragma unroll
-  for (int blk = 0; blk < V::BLOCKS; ++blk) {
-    if (blk) __syncthreads();
-    if (r < live) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int d = (4 * g + e) * V::DPL;
-        if (d < BD)
-#pragma unroll
-          for (int j = 0; j < V::DPL; ++j) lds_o[wave][d + j][r] = acc[blk * V::DPL + j][e];
-      }
-    }
-    __syncthreads();
-    if (blk == 0) {
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds_ml[w][h].x);
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float2 ml = lds_ml[w][h];
-        f[w] = part_factor(ml, top);
-        total += f[w] * ml.y;
-      }
-    }
-    for (int d = (threadIdx.x >> 4) * 8; h < live && d < BD; d += 4 * kWaves * 8) {
-      float x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) x[e] = fmaf(f[w], lds_o[w][d + e][h], x[e]);
-      }
-      if (part.count == 1) {
-        const float inv = value_factor<FMT>() / total;
-        u32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = total == 0.f ? 0 : cvt_pk_bf16(x[2 * e] * inv, x[2 * e + 1] * inv);  // (0 times x could be NaN)
-        *reinterpret_cast<u32x4 *>(o.out + head * HD + blk * BD + d) = v;
-      } else {
-        float *to = o.part_o + slot * HD + blk * BD + d;
-        *reinterpret_cast<f32x4 *>(to) = f32x4{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<f32x4 *>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
-      }
-    }
-  }
-  if (part.count > 1 && threadIdx.x < live) o.part_ml[slot] = make_float2(top, total);
+  finish_part<HD, V::DPL, V::BLOCKS>(o, part, acc, m, sum, value_factor<FMT>(), wave, live, head, slot, lds_o, lds_ml);
 }
 
 // What one launch of the kernel takes.

@@ -3,8 +3,256 @@
 
 namespace et {
 
+// Keys in 4 bits.  A lane's load serves several steps of 32 dimensions, and so does its exponent: where a row is a multiple of 128,
+// 32 dimensions (a block) for four steps, elsewhere 16 (half a block) for two, and the third step has the dimensions from 64 on.
+template <int HD>
+struct MxKeys {
+  using Lay = KvLayout<HD, ET_KV_MXFP4>;
+  static constexpr int STEPS = (HD + 31) / 32, NREG = STEPS;
+  static constexpr bool WIDE = HD % 128 == 0;
+  static constexpr int UNITS = WIDE ? STEPS / 4 : STEPS - 1;             // exponents of a lane
+  static __device__ __forceinline__ int dim(int s, int g) {
+    return WIDE ? s / 4 * 128 + g * 32 + s % 4 * 8 : s < 2 ? g * 16 + s * 8 : 64 + g * 8;
+  }
+  // Past the row's end the last dimensions are read again (and not used).
+  static __device__ __forceinline__ void load(const char *base, int r, int g, uint32_t (&w)[NREG]) {
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int i = 0; i < STEPS / 4; ++i) {
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(base + (uint32_t)(r * Lay::kRow + i * 64 + g * 16));
+        w[4 * i] = v[0], w[4 * i + 1] = v[1], w[4 * i + 2] = v[2], w[4 * i + 3] = v[3];
+      }
+    } else {
+      const uint2 v = *reinterpret_cast<const uint2 *>(base + (uint32_t)(r * Lay::kRow + g * 8));
+      w[0] = v.x, w[1] = v.y;
+      if constexpr (STEPS > 2) w[2] = *reinterpret_cast<const uint32_t *>(base + (uint32_t)(r * Lay::kRow + min(32 + g * 4, Lay::kRow - 4)));
+    }
+  }
+  static __device__ __forceinline__ void load_units(const char *exponents, int r, int g, uint32_t (&u)[UNITS]) {
+    const uint8_t *e = reinterpret_cast<const uint8_t *>(exponents) + (uint32_t)(r * Lay::kBlocks);
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) u[i] = (uint32_t)e[4 * i + g];
+    } else {
+      u[0] = (uint32_t)e[g / 2];
+      if constexpr (STEPS > 2) u[1] = (uint32_t)e[2];
+    }
+  }
+  static __device__ __forceinline__ u32x4 operand(const uint32_t (&w)[NREG], const uint32_t (&u)[UNITS], int s, int g) {
+    const u32x4 v = mx_decode8(w[s], u[WIDE ? s / 4 : s / 2]);
+    return HD % 32 && s == STEPS - 1 && 64 + g * 8 >= HD ? u32x4{0, 0, 0, 0} : v;
+  }
+};
+// Values in 4 bits: a lane's dimensions of a token are one load of 2 or 4 bytes, become bfloat16 pairs with the exponent of their block,
+// and go on as bfloat16 values do.
+template <int HD>
+struct MxValues {
+  using Lay = KvLayout<HD, ET_KV_MXFP4>;
+  using Wide = Values<HD, ET_KV_BF16>;
+  static constexpr int DPL = Wide::DPL, BLOCKS = Wide::BLOCKS, NREG = Wide::NREG;
+  // the codes of the lane's dimensions
+  static __device__ __forceinline__ uint32_t load(const char *base, int token, int r, int blk) {
+    const char *at = base + (uint32_t)(token * Lay::kRow + (blk * 128 + min(r, HD / DPL - 1) * DPL) / 2);
+    if constexpr (DPL == 8) return *reinterpret_cast<const uint32_t *>(at);
+    else return *reinterpret_cast<const uint16_t *>(at);
+  }
+  // the exponents of four tokens from `token` on, a byte each
+  static __device__ __forceinline__ uint32_t load_units(const char *exponents, int page_size, int token, int r, int blk) {
+    const int block = blk * 4 + min(r, HD / DPL - 1) * DPL / kMxBlock;
+    return *reinterpret_cast<const uint32_t *>(exponents + (uint32_t)(block * page_size + token));
+  }
+  // token e of those four (its exponent moves to where float32 has it; what comes along does not count)
+  static __device__ __forceinline__ void widen(uint32_t code, uint32_t units, int e, uint32_t (&w)[NREG]) {
+    const uint32_t unit = e == 0 ? units << 23 : e == 1 ? units << 15 : e == 2 ? units << 7 : units >> 1;
+    w[0] = mx_pair<0>(code, unit), w[1] = mx_pair<1>(code, unit);
+    if constexpr (DPL == 8) w[2] = mx_pair<2>(code, unit), w[3] = mx_pair<3>(code, unit);
+  }
+  static __device__ __forceinline__ u32x4 operand(const uint32_t (&w)[8][NREG], int j) { return Wide::operand(w, j); }
+};
+
+// Largest of three (without the canonicalisation that fmaxf asks for: these are results of arithmetic).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+// As paged_attention_kernel: a workgroup takes one part of a sequence's tokens for up to 16 query heads of one key-value head, its
+// wavefronts tiles of 32 tokens in turn, S^T = K Q^T and O^T += V^T P^T by matrix instructions on bfloat16 numbers, which codes and their power of two
+// are exactly; a weight is the sum of two of them.  A tile's registers are loaded again as soon as they have become operands, so the next
+// tile's keys come in during the softmax and the second product, its values during that and the next logits.
+template <int HD, bool ONE>
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_mxfp4_kernel(const int32_t *len, const int32_t *table, int n_seqs, int share, int bound,
+                                                                 int window, int units, int row_tiles, int page_shift, int table_stride,
+                                                                 int group, PagedMore o) {
+  using Lay = KvLayout<HD, ET_KV_MXFP4>;
+  using K = MxKeys<HD>;
+  using V = MxValues<HD>;
+  constexpr int ACC = V::BLOCKS * V::DPL;
+  __shared__ float lds_o[kWaves][HD / V::BLOCKS][16];
+  __shared__ float2 lds_ml[kWaves][16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const PagedArgs a{len, n_seqs, bound, window, share};
+  // (row tiles of one part and key-value head eight workgroups apart, as there)
+  const int kv_heads = units / row_tiles;
+  int place = blockIdx.x, rt = 0;
+  if (row_tiles > 1) {
+    const int turn = 8 * row_tiles, first = place / turn * 8, width = min(8, (int)gridDim.x / row_tiles - first);
+    rt = place % turn / width;
+    place = first + place % turn % width;
+  }
+  const int item = place / kv_heads, kv = place % kv_heads;
+  const int n_heads = group * kv_heads, ps = 1 << page_shift;
+  const int live = min(16, group - rt * 16);              // query heads of this workgroup
+  Part part{item, 0, 1, 0, 0, 0};
+  if (a.share) {
+    part = find_part<ONE>(a, item, -1);
+    if (part.seq < 0) return;
+  } else {
+    part.len = a.len[item];
+  }
+  const int b = __builtin_amdgcn_readfirstlane(part.seq);
+  const SeqRange sr(__builtin_amdgcn_readfirstlane(part.len), a.bound, a.window);
+  const int start = sr.lo + part.index * (int)part.per * kBlock;
+  const int end = a.share ? (int)min((int64_t)sr.hi, (int64_t)start + (int64_t)part.per * kBlock) : sr.hi;
+  const int tiles = end > start ? (end - start + kTile - 1) / kTile : 0;
+
+  f32x4 acc[ACC];
+#pragma unroll
+  for (int j = 0; j < ACC; ++j) acc[j] = f32x4{0, 0, 0, 0};
+  float m = -INFINITY, sum = 0.f;                         // of query head r; sum: this lane's tokens only
+
+  const int32_t *row = table + (int64_t)b * table_stride;
+  int page_of = -1;                                       // lane i: page of the wavefront's i-th group of 16 tokens, of 64
+  auto fetch_pages = [&](int t) {
+    const int pos = start + (t + (lane >> 1) * kWaves) * kTile + (lane & 1) * 16;
+    page_of = pos < end ? row[pos >> page_shift] : -1;
+    if (page_of >= o.n_pages) page_of = -1;
+  };
+  // (A group without a page reads the first page's bytes, and its tokens do not count.)
+  auto head_of = [&](int page) { return o.data + max(page, 0) * o.page_bytes + (int64_t)kv * Lay::head_bytes(ps); };
+  uint32_t kw[2][K::NREG], ku[2][K::UNITS], code[V::BLOCKS][8], vu[V::BLOCKS][2];
+  int page[2];                                            // of the tile whose keys are here
+  auto load_keys = [&](int t, int i) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      page[u] = __builtin_amdgcn_readlane(page_of, i + u);
+      const int at = (start + t * kTile + 16 * u) & (ps - 1);
+      const char *head = head_of(page[u]);
+      K::load(head + at * Lay::kRow, r, g, kw[u]);
+      K::load_units(head + Lay::key_scale(ps) + at * Lay::kBlocks, r, g, ku[u]);
+    }
+  };
+  auto load_values = [&](int t, int blk) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int at = (start + t * kTile + 16 * u) & (ps - 1);
+      const char *head = head_of(page[u]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) code[blk][4 * u + e] = V::load(head + Lay::values(ps) + at * Lay::kRow, 4 * g + e, r, blk);
+      vu[blk][u] = V::load_units(head + Lay::value_scale(ps), ps, at + 4 * g, r, blk);
+    }
+  };
+  fetch_pages(wave);                                      // (in front of the queries' loads: the keys' wait for it)
+  u32x4 qf[K::STEPS];
+#pragma unroll
+  for (int st = 0; st < K::STEPS; ++st) {
+    const int d = K::dim(st, g);
+    qf[st] = u32x4{0, 0, 0, 0};
+    if (r < live && d < HD)
+      qf[st] = *reinterpret_cast<const u32x4 *>(o.q + b * o.q_stride + ((int64_t)kv * group + rt * 16 + r) * HD + d);
+  }
+  if (wave < tiles) {
+    load_keys(wave, 0);
+#pragma unroll
+    for (int blk = 0; blk < V::BLOCKS; ++blk) load_values(wave, blk);
+  }
+  for (int t = wave, i = 0; t < tiles; t += kWaves) {
+    const int pos0 = start + t * kTile;
+    // tokens that do not count: no page, past the end, before the window
+    const bool paged[2] = {page[0] >= 0, page[1] >= 0};
+    const bool whole = paged[0] && paged[1] && pos0 >= sr.first && pos0 + kTile <= end, more = t + kWaves < tiles;
+    float z[8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x4 d{0, 0, 0, 0};
+#pragma unroll
+      for (int st = 0; st < K::STEPS; ++st) d = mfma16(K::operand(kw[u], ku[u], st, g), qf[st], d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[4 * u + e] = whole_product(d[e], o.scale_log2);
+    }
+    i = (i + 2) & 63;
+    if (i == 0) fetch_pages(t + kWaves);
+    if (more) load_keys(t + kWaves, i);
+    uint32_t dead = 0;
+    if (!whole) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int pos = pos0 + 16 * (e / 4) + 4 * g + (e & 3);
+        if (!paged[e / 4] || pos < sr.first || pos >= end) {
+          dead |= 1u << e;
+          z[e] = -INFINITY;
+        }
+      }
+    }
+    // The reference of the exponentials moves when a logit exceeds it by 2^8: below that nothing overflows.
+    float top = max3(max3(z[0], z[1], z[2]), max3(z[3], z[4], z[5]), max3(z[6], z[7], z[7]));
+    if (__ballot(top > m + 8.f)) {
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float m2 = fmaxf(m, top), f = m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m2);
+      m = m2;
+      sum *= f;
+#pragma unroll
+      for (int j = 0; j < ACC; ++j) acc[j] *= f;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    float p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(z[e] - ref);
+      sum += p[e];
+    }
+    // the weights' halves: what bfloat16 cuts off goes into the second
+    u32x4 pf, pl;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      pf[e] = __builtin_amdgcn_perm(__float_as_uint(p[2 * e + 1]), __float_as_uint(p[2 * e]), 0x07060302u);
+      pl[e] = cvt_pk_bf16(p[2 * e] - bf16lo_to_f32(pf[e]), p[2 * e + 1] - bf16hi_to_f32(pf[e]));
+    }
+#pragma unroll
+    for (int blk = 0; blk < V::BLOCKS; ++blk) {
+      uint32_t vw[8][V::NREG];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) V::widen(code[blk][e], vu[blk][e / 4], e & 3, vw[e]);
+      if (more) load_values(t + kWaves, blk);
+      if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int x = 0; x < V::NREG; ++x) vw[e][x] = dead >> e & 1 ? 0 : vw[e][x];     // (0 times what lies there could be NaN)
+      }
+#pragma unroll
+      for (int j = 0; j < V::DPL; ++j) {
+        const u32x4 values = V::operand(vw, j);
+        f32x4 &to = acc[blk * V::DPL + j];
+        to = mfma16(values, pf, mfma16(values, pl, to));
+      }
+    }
+  }
+  const int h = threadIdx.x & 15;
+  const int64_t head = (int64_t)b * n_heads + (int64_t)kv * group + rt * 16 + h;
+  const int64_t slot = (int64_t)item * n_heads + kv * group + rt * 16 + h;       // of a part that is one of several
+  finish_part<HD, V::DPL, V::BLOCKS>(o, part, acc, m, sum, 1.f, wave, live, head, slot, lds_o, lds_ml);
+}
+
 int launch_paged_mxfp4(int head_dim, const PagedLaunch &l) {
-  return kv_dispatch_mxfp4(head_dim, [&](auto hd) { return launch_paged<hd.value, ET_KV_MXFP4>(l); });
+  return kv_dispatch_mxfp4(head_dim, [&](auto hd) {
+    (l.n_seqs == 1 ? paged_mxfp4_kernel<hd.value, true> : paged_mxfp4_kernel<hd.value, false>)<<<l.blocks, 64 * kWaves, 0, l.stream>>>(
+        l.len, l.table, l.n_seqs, l.share, l.bound, l.window, l.units, l.row_tiles, l.page_shift, l.table_stride, l.group, l.more);
+    ET_LAUNCH_CHECK();
+    return ET_OK;
+  });
 }
 
 }  // namespace et
