@@ -804,19 +804,20 @@ class PagePool(_OnDevice):
         if rows < 0 or rows > _INT_MAX:
             raise ValueError("rows = %d must be in [0, 2^31 - 1]" % rows)
         if out is None:
-            cu = torch.empty(n + 1, dtype=torch.int32, device=self.device)
-            out = cu, torch.empty(rows, dtype=torch.int32, device=self.device), torch.empty(rows, dtype=torch.int64, device=self.device)
+            out = cu, positions, slots = kv_len.new_empty(n + 1), kv_len.new_empty(rows), kv_len.new_empty(rows, dtype=torch.int64)
         else:
+            cu, positions, slots = out
             if not all(t.is_contiguous() and t.device == self.device for t in out) or \
                     [t.dtype for t in out] != [torch.int32, torch.int32, torch.int64] or \
-                    out[0].shape != (n + 1,) or out[1].numel() < rows or out[2].numel() < rows:
+                    cu.shape != (n + 1,) or positions.numel() < rows or slots.numel() < rows:
                 raise ValueError("out must be cu_rows int32 [%d], positions int32 and slots int64 [%d], contiguous, on %s" % (n + 1, rows, self.device))
-        need = self._lib.et_kv_resize_workspace_bytes(n, rows)
+        lib = self._lib
+        # (no workspace up to 1024 sequences and 8192 rows)
+        need = lib.et_kv_resize_workspace_bytes(n, rows) if n > 1024 or rows > 8192 else 0
         ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-        cu, positions, slots = out
-        _check(self._lib.et_kv_resize(self._pool, self.state.data_ptr(), state_out.data_ptr(), page_table.data_ptr(), strides[0] if n > 1 else pages,
-                                      pages, kv_len.data_ptr(), new_len.data_ptr(), n, rows, cu.data_ptr(), positions.data_ptr(),
-                                      slots.data_ptr(), ws.data_ptr() if need else None, need, s))
+        _check(lib.et_kv_resize(self._pool, self.state.data_ptr(), state_out.data_ptr(), page_table.data_ptr(), strides[0] if n > 1 else pages,
+                                pages, kv_len.data_ptr(), new_len.data_ptr(), n, rows, cu.data_ptr(), positions.data_ptr(),
+                                slots.data_ptr(), ws.data_ptr() if need else None, need, s))
         return out
 
     def _ints(self, t, name):
@@ -879,33 +880,46 @@ class Rotary(_OnDevice):
                 return self.apply(q, k, positions, out, transpose)
         if not (isinstance(positions, torch.Tensor) and positions.dtype is torch.int32 and positions.device == self.device):
             raise TypeError("positions must be an int32 tensor on %s" % self.device)
-        rows = positions.shape[0] if positions.dim() == 1 else -1
-        if rows < 0 or not positions.is_contiguous():
+        rows = positions.shape
+        if len(rows) != 1 or not positions.is_contiguous():
             raise ValueError("positions must be contiguous, one for each row")
-        out = (None, None) if out is None else out
-        q_out, q_rows = self._turned(q, out[0], "q", rows)
-        k_out, k_rows = (None, None) if k is None else self._turned(k, out[1], "k", rows)
-        _check(self._lib.et_rotary_apply(self._rotary, positions.data_ptr(), rows, q_rows, k_rows, int(bool(transpose)), s))
+        rows, d = rows[0], self.head_dim
+        at, heads, stride = self._heads(q, "q", rows, d)
+        if out is None or out[0] is None:
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            q_rows = _RotaryRows(at, stride, q_out.data_ptr(), heads * d, heads)
+        else:
+            q_out = out[0]
+            q_rows = self._out(q, q_out, "out of q", rows, at, heads, stride)
+        k_out = k_rows = None
+        if k is not None:
+            at, heads, stride = self._heads(k, "k", rows, d)
+            if out is None or out[1] is None:
+                k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+                k_rows = _RotaryRows(at, stride, k_out.data_ptr(), heads * d, heads)
+            else:
+                k_out = out[1]
+                k_rows = self._out(k, k_out, "out of k", rows, at, heads, stride)
+        _check(self._lib.et_rotary_apply(self._rotary, positions.data_ptr(), rows, q_rows, k_rows, 1 if transpose else 0, s))
         return q_out, k_out
 
-    def _turned(self, x, out, name, rows):
-        ptr, heads, stride = self._heads(x, name, rows)
-        if out is None:
-            out = torch.empty_like(x, memory_format=torch.contiguous_format)
-            return out, _RotaryRows(ptr, stride, out.data_ptr(), heads * self.head_dim, heads)
-        to, to_heads, to_stride = self._heads(out, "out of " + name, rows)
+    def _out(self, x, out, name, rows, at, heads, stride):
+        if out is x:
+            return _RotaryRows(at, stride, at, stride, heads)
+        to, to_heads, to_stride = self._heads(out, name, rows, self.head_dim)
         if to_heads != heads:
-            raise ValueError("%s has %d heads, its out %d" % (name, heads, to_heads))
-        return out, _RotaryRows(ptr, stride, to, to_stride, heads)
+            raise ValueError("%s has %d heads instead of %d" % (name, to_heads, heads))
+        return _RotaryRows(at, stride, to, to_stride, heads)
 
-    def _heads(self, t, name, rows):
+    def _heads(self, t, name, rows, d):
+        """(address, heads, row stride) of [rows, heads * d] or [rows, heads, d] with contiguous rows."""
         if not (isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.device == self.device):
             raise TypeError("%s must be a bfloat16 tensor on %s" % (name, self.device))
-        shape, strides, d = t.shape, t.stride(), self.head_dim
-        if len(shape) == 3 and shape[2] == d and strides[2] == 1 and (strides[1] == d or shape[1] == 1):
-            heads = shape[1]
-        elif len(shape) == 2 and strides[1] == 1 and shape[1] % d == 0:
+        shape, strides = t.shape, t.stride()
+        if len(shape) == 2 and strides[1] == 1 and shape[1] % d == 0:
             heads = shape[1] // d
+        elif len(shape) == 3 and shape[2] == d and strides[2] == 1 and (strides[1] == d or shape[1] == 1):
+            heads = shape[1]
         else:
             raise ValueError("%s must be [rows, heads * %d] or [rows, heads, %d] with contiguous rows" % (name, d, d))
         if shape[0] != rows:

@@ -123,75 +123,81 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_mxfp4_kernel(const int32
   float m = -INFINITY, sum = 0.f;                         // of query head r; sum: this lane's tokens only
 
   const int32_t *row = table + (int64_t)b * table_stride;
-  int page_of = -1;                                       // lane i: page of the wavefront's i-th group of 16 tokens, of 64
-  auto fetch_pages = [&](int t) {
-    const int pos = start + (t + (lane >> 1) * kWaves) * kTile + (lane & 1) * 16;
-    page_of = pos < end ? row[pos >> page_shift] : -1;
-    if (page_of >= o.n_pages) page_of = -1;
-  };
-  // (A group without a page reads the first page's bytes, and its tokens do not count.)
+  const int mine = (tiles - wave + kWaves - 1) / kWaves;  // tiles of this wavefront
+  int page_of = -1;                                       // lane i: page of the i-th group of 16 tokens of 32 tiles of the wavefront
+  // (A group of 16 tokens without a page reads the first page's bytes, and its tokens do not count.)
   auto head_of = [&](int page) { return o.data + max(page, 0) * o.page_bytes + (int64_t)kv * Lay::head_bytes(ps); };
-  uint32_t kw[2][K::NREG], ku[2][K::UNITS], code[V::BLOCKS][8], vu[V::BLOCKS][2];
-  int page[2];                                            // of the tile whose keys are here
-  auto load_keys = [&](int t, int i) {
+  struct Tile {
+    uint32_t kw[2][K::NREG], ku[2][K::UNITS], code[V::BLOCKS][8], vu[V::BLOCKS][2];
+    int page[2];
+  };
+  Tile x;
+  auto load_keys = [&](int n) {                         // of the wavefront's n-th tile
+    const int t = wave + n * kWaves;
+    if ((n & 31) == 0) {
+      const int pos = start + (t + (lane >> 1) * kWaves) * kTile + (lane & 1) * 16;
+      page_of = pos < end ? row[pos >> page_shift] : -1;
+      if (page_of >= o.n_pages) page_of = -1;
+    }
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      page[u] = __builtin_amdgcn_readlane(page_of, i + u);
+      x.page[u] = __builtin_amdgcn_readlane(page_of, 2 * (n & 31) + u);
       const int at = (start + t * kTile + 16 * u) & (ps - 1);
-      const char *head = head_of(page[u]);
-      K::load(head + at * Lay::kRow, r, g, kw[u]);
-      K::load_units(head + Lay::key_scale(ps) + at * Lay::kBlocks, r, g, ku[u]);
+      const char *head = head_of(x.page[u]);
+      K::load(head + at * Lay::kRow, r, g, x.kw[u]);
+      K::load_units(head + Lay::key_scale(ps) + at * Lay::kBlocks, r, g, x.ku[u]);
     }
   };
-  auto load_values = [&](int t, int blk) {
+  auto load_values = [&](int n, int blk) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int at = (start + t * kTile + 16 * u) & (ps - 1);
-      const char *head = head_of(page[u]);
+      const int at = (start + (wave + n * kWaves) * kTile + 16 * u) & (ps - 1);
+      const char *head = head_of(x.page[u]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) code[blk][4 * u + e] = V::load(head + Lay::values(ps) + at * Lay::kRow, 4 * g + e, r, blk);
-      vu[blk][u] = V::load_units(head + Lay::value_scale(ps), ps, at + 4 * g, r, blk);
+      for (int i = 0; i < 4; ++i) x.code[blk][4 * u + i] = V::load(head + Lay::values(ps) + at * Lay::kRow, 4 * g + i, r, blk);
+      x.vu[blk][u] = V::load_units(head + Lay::value_scale(ps), ps, at + 4 * g, r, blk);
     }
   };
-  fetch_pages(wave);                                      // (in front of the queries' loads: the keys' wait for it)
+  // (no branches around these loads, and the queries' awaited here: a turn then waits for its own operands alone)
   u32x4 qf[K::STEPS];
 #pragma unroll
-  for (int st = 0; st < K::STEPS; ++st) {
-    const int d = K::dim(st, g);
-    qf[st] = u32x4{0, 0, 0, 0};
-    if (r < live && d < HD)
-      qf[st] = *reinterpret_cast<const u32x4 *>(o.q + b * o.q_stride + ((int64_t)kv * group + rt * 16 + r) * HD + d);
-  }
-  if (wave < tiles) {
-    load_keys(wave, 0);
+  for (int st = 0; st < K::STEPS; ++st)
+    qf[st] = *reinterpret_cast<const u32x4 *>(o.q + b * o.q_stride + ((int64_t)kv * group + rt * 16 + min(r, live - 1)) * HD +
+                                              min(K::dim(st, g), HD - 8));
+  if (mine > 0) {
+    load_keys(0);
 #pragma unroll
-    for (int blk = 0; blk < V::BLOCKS; ++blk) load_values(wave, blk);
+    for (int blk = 0; blk < V::BLOCKS; ++blk) load_values(0, blk);
   }
-  for (int t = wave, i = 0; t < tiles; t += kWaves) {
-    const int pos0 = start + t * kTile;
+#pragma unroll
+  for (int st = 0; st < K::STEPS; ++st) {
+    asm volatile("" : "+v"(qf[st]));
+    if (r >= live || K::dim(st, g) >= HD) qf[st] = u32x4{0, 0, 0, 0};
+  }
+  for (int n = 0; n < mine; ++n) {
+    const int pos0 = start + (wave + n * kWaves) * kTile;
     // tokens that do not count: no page, past the end, before the window
-    const bool paged[2] = {page[0] >= 0, page[1] >= 0};
-    const bool whole = paged[0] && paged[1] && pos0 >= sr.first && pos0 + kTile <= end, more = t + kWaves < tiles;
+    const bool paged[2] = {x.page[0] >= 0, x.page[1] >= 0};
+    const bool whole = paged[0] && paged[1] && pos0 >= sr.first && pos0 + kTile <= end;
+    const int next = min(n + 1, mine - 1);              // (the last tile again, from the caches, so that every turn has the same loads)
     float z[8];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       f32x4 d{0, 0, 0, 0};
 #pragma unroll
-      for (int st = 0; st < K::STEPS; ++st) d = mfma16(K::operand(kw[u], ku[u], st, g), qf[st], d);
+      for (int st = 0; st < K::STEPS; ++st) d = mfma16(K::operand(x.kw[u], x.ku[u], st, g), qf[st], d);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) z[4 * u + e] = whole_product(d[e], o.scale_log2);
+      for (int i = 0; i < 4; ++i) z[4 * u + i] = whole_product(d[i], o.scale_log2);
     }
-    i = (i + 2) & 63;
-    if (i == 0) fetch_pages(t + kWaves);
-    if (more) load_keys(t + kWaves, i);
+    load_keys(next);
     uint32_t dead = 0;
     if (!whole) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int pos = pos0 + 16 * (e / 4) + 4 * g + (e & 3);
-        if (!paged[e / 4] || pos < sr.first || pos >= end) {
-          dead |= 1u << e;
-          z[e] = -INFINITY;
+      for (int i = 0; i < 8; ++i) {
+        const int pos = pos0 + 16 * (i / 4) + 4 * g + (i & 3);
+        if (!paged[i / 4] || pos < sr.first || pos >= end) {
+          dead |= 1u << i;
+          z[i] = -INFINITY;
         }
       }
     }
@@ -209,28 +215,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_mxfp4_kernel(const int32
     const float ref = m == -INFINITY ? 0.f : m;
     float p[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(z[e] - ref);
-      sum += p[e];
+    for (int i = 0; i < 8; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(z[i] - ref);
+      sum += p[i];
     }
     // the weights' halves: what bfloat16 cuts off goes into the second
     u32x4 pf, pl;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      pf[e] = __builtin_amdgcn_perm(__float_as_uint(p[2 * e + 1]), __float_as_uint(p[2 * e]), 0x07060302u);
-      pl[e] = cvt_pk_bf16(p[2 * e] - bf16lo_to_f32(pf[e]), p[2 * e + 1] - bf16hi_to_f32(pf[e]));
+    for (int i = 0; i < 4; ++i) {
+      pf[i] = __builtin_amdgcn_perm(__float_as_uint(p[2 * i + 1]), __float_as_uint(p[2 * i]), 0x07060302u);
+      pl[i] = cvt_pk_bf16(p[2 * i] - bf16lo_to_f32(pf[i]), p[2 * i + 1] - bf16hi_to_f32(pf[i]));
     }
 #pragma unroll
     for (int blk = 0; blk < V::BLOCKS; ++blk) {
       uint32_t vw[8][V::NREG];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) V::widen(code[blk][e], vu[blk][e / 4], e & 3, vw[e]);
-      if (more) load_values(t + kWaves, blk);
+      for (int i = 0; i < 8; ++i) V::widen(x.code[blk][i], x.vu[blk][i / 4], i & 3, vw[i]);
+      load_values(next, blk);
       if (!whole) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int x = 0; x < V::NREG; ++x) vw[e][x] = dead >> e & 1 ? 0 : vw[e][x];     // (0 times what lies there could be NaN)
+          for (int j = 0; j < V::NREG; ++j) vw[i][j] = dead >> i & 1 ? 0 : vw[i][j];   // (0 times what lies there could be NaN)
       }
 #pragma unroll
       for (int j = 0; j < V::DPL; ++j) {
