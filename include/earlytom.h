@@ -444,13 +444,13 @@ int et_attention_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, const u
  * pages are missing.  A page must be in one place, a table's live entry or a free cell of the ring; sequences that share pages are the
  * caller's to keep apart.  Whatever state, ring, lengths and table hold, nothing outside them is touched.
  * state_dev and state_out_dev int32 [4], aligned to 16 bytes; n_seqs at most 2^20, n_seqs * pages_per_seq below 2^31.  workspace:
- * et_kv_resize_workspace_bytes (0 up to 1024 sequences and 8192 rows), aligned to 16 bytes, contents arbitrary.  Calls on the same ring,
+ * et_kv_resize_workspace_bytes (0 up to 4096 sequences), aligned to 16 bytes, contents arbitrary.  Calls on the same ring,
  * state or table follow each other in one stream.  Asynchronous on `hip_stream`; can be captured.  Errors: INVALID_ARG, WORKSPACE, HIP. */
 typedef struct {
   int32_t *ring_dev;           /* [n_pages]                                                          */
   int32_t n_pages, page_size;  /* page_size 16, 32, 64, 128 or 256                                   */
 } et_kv_pool;
-size_t et_kv_resize_workspace_bytes(int32_t n_seqs, int32_t rows);
+size_t et_kv_resize_workspace_bytes(int32_t n_seqs);
 int et_kv_resize(const et_kv_pool *pool, const int32_t *state_dev, int32_t *state_out_dev, int32_t *page_table_dev,
                  int32_t table_stride, int32_t pages_per_seq, const int32_t *kv_len_dev, const int32_t *new_len_dev,
                  int32_t n_seqs, int32_t rows, int32_t *cu_rows_dev, int32_t *positions_dev, int64_t *slots_dev,

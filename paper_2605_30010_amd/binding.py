@@ -140,7 +140,7 @@ def load_library():
         "et_kv_page_bytes": (sz, [i32, i32, i32, i32]),
         "et_kv_append": (C.c_int, [C.POINTER(_KvCache), C.POINTER(_KvSeqs), vp, i32, vp, i64, vp, i64, vp]),
         "et_kv_append_slots": (C.c_int, [C.POINTER(_KvCache), vp, i32, vp, i64, vp, i64, vp]),
-        "et_kv_resize_workspace_bytes": (sz, [i32, i32]),
+        "et_kv_resize_workspace_bytes": (sz, [i32]),
         "et_kv_resize": (C.c_int, [C.POINTER(_KvPool), vp, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]),
         "et_rotary_steps": (C.c_int, [C.POINTER(_RotaryScaling), i32, C.c_double, C.POINTER(C.c_uint64), _FP]),
         "et_rotary_apply": (C.c_int, [C.POINTER(_Rotary), vp, i32, C.POINTER(_RotaryRows), C.POINTER(_RotaryRows), i32, vp]),
@@ -812,8 +812,7 @@ class PagePool(_OnDevice):
                     cu.shape != (n + 1,) or positions.numel() < rows or slots.numel() < rows:
                 raise ValueError("out must be cu_rows int32 [%d], positions int32 and slots int64 [%d], contiguous, on %s" % (n + 1, rows, self.device))
         lib = self._lib
-        # (no workspace up to 1024 sequences and 8192 rows)
-        need = lib.et_kv_resize_workspace_bytes(n, rows) if n > 1024 or rows > 8192 else 0
+        need = lib.et_kv_resize_workspace_bytes(n) if n > 4096 else 0                # (none up to 4096 sequences)
         ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
         _check(lib.et_kv_resize(self._pool, self.state.data_ptr(), state_out.data_ptr(), page_table.data_ptr(), strides[0] if n > 1 else pages,
                                 pages, kv_len.data_ptr(), new_len.data_ptr(), n, rows, cu.data_ptr(), positions.data_ptr(),

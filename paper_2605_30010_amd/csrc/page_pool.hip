@@ -33,22 +33,16 @@ struct PoolState {
 };
 
 constexpr int kPoolThreads = 1024, kPoolWaves = kPoolThreads / 64;
-constexpr int kOneSeqs = 1024;                           // sequences and rows up to which one workgroup does everything
-constexpr int kOneRows = 8192;
 
-// Sums over the workgroup's threads before mine of three numbers, and the totals.  The first may pass 32 bits.
+// Sums over the workgroup's threads before mine of three numbers, and the totals.  The first may pass 32 bits: its halves are added apart.
 struct Triple {
   int64_t rows;
   int grow, shrink;
 };
 __device__ __forceinline__ Triple scan_threads(Triple mine, Triple &total, Triple (&lds)[kPoolWaves]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t r = mine.rows;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t up = __shfl_up(r, d, 64);
-    if (lane >= d) r += up;
-  }
+  const int low = wave_inclusive_scan((int)(mine.rows & 0xFFFF)), high = wave_inclusive_scan((int)(mine.rows >> 16));
+  const int64_t r = ((int64_t)high << 16) + low;
   const int g = wave_inclusive_scan(mine.grow), s = wave_inclusive_scan(mine.shrink);
   if (lane == 63) lds[wave] = {r, g, s};
   __syncthreads();
@@ -59,7 +53,6 @@ __device__ __forceinline__ Triple scan_threads(Triple mine, Triple &total, Tripl
     if (w == wave) before = total;
     total.rows += lds[w].rows, total.grow += lds[w].grow, total.shrink += lds[w].shrink;
   }
-  __syncthreads();                                       // (the sums may be written again)
   return {before.rows + r - mine.rows, before.grow + g - mine.grow, before.shrink + s - mine.shrink};
 }
 __device__ __forceinline__ int clipped(int64_t rows) { return (int)min(rows, (int64_t)INT32_MAX); }
@@ -74,88 +67,149 @@ __device__ __forceinline__ int find_seq(const int *first, int lo, int hi, int x)
   return lo;
 }
 
-// Gives the pages behind the sequences' ends back: entry i of all `total` goes, if it is a page, behind the ring's `count` free ones,
-// in order.  By one workgroup; returns how many found room there.
-__device__ __forceinline__ int give_back(const PoolArgs &a, PoolState st, const int *shrink_first, int total, int *lds) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, room = a.n_pages - st.count;
-  int given = 0;
-  for (int base = 0; base < total; base += kPoolThreads) {
-    const int i = base + threadIdx.x;
-    int page = -1;
-    if (i < total) {
-      const int b = find_seq(shrink_first, 0, a.n_seqs - 1, i);
-      page = a.table[(int64_t)b * a.table_stride + a.pages(max(a.new_len[b], 0)) + (i - shrink_first[b])];
-    }
-    const bool good = a.is_page(page);
-    const uint64_t votes = __ballot(good);
-    if (lane == 0) lds[wave] = __popcll(votes);
-    __syncthreads();
-    int at = given + __popcll(votes & ((1ull << lane) - 1));
-#pragma unroll
-    for (int w = 0; w < kPoolWaves; ++w) {
-      const int n = lds[w];
-      if (w < wave) at += n;
-      given += n;
-    }
-    if (good && at < room) a.ring[a.cell(st.head, st.count + at)] = page;
-    __syncthreads();
+// The same for all lanes of a wavefront together, 64 probes at a time.
+__device__ __forceinline__ int find_seq_all(const int *first, int from, int n_seqs, int x) {
+  const int lane = threadIdx.x & 63;
+  int len = n_seqs - from;                               // the answer is in [from, from + len)
+  while (len > 1) {
+    const int step = (len + 63) / 64, i = from + lane * step;
+    const int hits = __popcll(__ballot(lane * step < len && first[min(i, n_seqs - 1)] <= x));
+    from += (hits - 1) * step;
+    len = min(step, n_seqs - from);
   }
-  return min(given, room);
+  return from;
+}
+// Gives pages behind sequences' ends back: of all `total` entries the workgroup takes 4096 from `back` on, a wavefront 256 neighbours (their
+// sequences lie between the first one's and the last one's).  Those that are pages go behind the ring's `count` free ones and the
+// `given` before them, in order.
+template <typename NewLength>
+__device__ __forceinline__ void give_pages(const PoolArgs &a, PoolState st, const int *shrink_first, int64_t back, int total, NewLength new_of,
+                                           int &given, int (&lds)[kPoolWaves]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, room = a.n_pages - st.count;
+  const int64_t k0 = back + wave * 256;
+  int page[4], mine = 0;
+  uint64_t votes[4] = {};
+  if (k0 < total) {
+    const int lo = find_seq_all(shrink_first, 0, a.n_seqs, (int)k0), hi = find_seq_all(shrink_first, lo, a.n_seqs, (int)min(k0 + 255, total - 1ll));
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t k = k0 + u * 64 + lane;
+      page[u] = -1;
+      if (k < total) {
+        const int b = find_seq(shrink_first, lo, hi, (int)k);
+        page[u] = a.table[(int64_t)b * a.table_stride + a.pages(new_of(b)) + ((int)k - shrink_first[b])];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) mine += __popcll(votes[u] = __ballot(a.is_page(page[u])));
+  }
+  if (lane == 0) lds[wave] = mine;
+  __syncthreads();
+  int at = given;
+#pragma unroll
+  for (int w = 0; w < kPoolWaves; ++w) {
+    const int n = lds[w];
+    if (w < wave) at += n;
+    given += n;
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int to = at + __popcll(votes[u] & ((1ull << lane) - 1));
+    if ((votes[u] >> lane & 1) && to < room) a.ring[a.cell(st.head, st.count + to)] = page[u];
+    at += __popcll(votes[u]);
+  }
+  __syncthreads();
 }
 // Entry i of all that are wanted: the ring's i-th page, or none.
 __device__ __forceinline__ int taken_page(const PoolArgs &a, PoolState st, int i) { return i < st.count ? a.ring[a.cell(st.head, i)] : -1; }
 
 __device__ __forceinline__ void leave_state(const PoolArgs &a, PoolState st, int wanted, int given, int32_t *state_out) {
   const int used = min(wanted, st.count);
-  *reinterpret_cast<int4 *>(state_out) = make_int4((int)(((uint32_t)st.head + (uint32_t)used) % (uint32_t)a.n_pages), st.count - used + given,
-                                                   wanted - used, 0);
+  *reinterpret_cast<int4 *>(state_out) = make_int4((int)(((uint32_t)st.head + (uint32_t)used) % (uint32_t)a.n_pages),
+                                                   st.count - used + min(given, a.n_pages - st.count), wanted - used, 0);
 }
 // Place of token `pos` whose page is `page`.
 __device__ __forceinline__ int64_t slot_of(const PoolArgs &a, int page, int pos) {
   return a.is_page(page) ? ((int64_t)page << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) : -1;
 }
 
-// Everything by one workgroup: up to 1024 sequences (a lane each) and a decoding step's rows.
-__global__ __launch_bounds__(kPoolThreads) void pool_step_kernel(const int32_t *state, const int32_t *len, const int32_t *new_len, int rows,
-                                                                PoolArgs a, int32_t *state_out, int32_t *cu, int32_t *positions,
-                                                                int64_t *slots) {
+// Up to 1024 PER sequences: every workgroup adds up all of them by itself, PER to a lane, and keeps the sums in LDS; then lanes take entries and
+// rows and look their sequence up there.  kFill: tables, positions, places and row ranges; kGive: pages given back and the new state, by one
+// workgroup.  Both in one for a decoding step (a single workgroup); otherwise the first of many gives and the others fill, or, where the new
+// state takes the old one's place, which the others read, a launch of its own gives.  The loads of a turn are issued together.
+constexpr int kGive = 1, kFill = 2;
+template <int PER>
+__global__ __launch_bounds__(kPoolThreads) void pool_resize_kernel(const int32_t *state, const int32_t *len, const int32_t *new_len, int rows,
+                                                                  int what, PoolArgs a, int32_t *state_out, int32_t *cu, int32_t *positions,
+                                                                  int64_t *slots) {
+  constexpr int kSeqs = PER * kPoolThreads;
   __shared__ Triple lds_sum[kPoolWaves];
-  __shared__ int row_first[kOneSeqs], grow_first[kOneSeqs], shrink_first[kOneSeqs], old_len[kOneSeqs], lds_votes[kPoolWaves];
+  __shared__ int row_first[kSeqs], grow_first[kSeqs], shrink_first[kSeqs], lds_given[kPoolWaves];
+  __shared__ int2 lds_len[PER == 1 ? kSeqs : 1];          // old and new (of more sequences they are fetched again)
   const int t = threadIdx.x;
   const PoolState st(state, a.n_pages);
-  int old = 0, fresh = 0;
-  if (t < a.n_seqs) old = max(len[t], 0), fresh = max(new_len[t], 0);
-  const int p0 = a.pages(old), p1 = a.pages(fresh);
-  Triple total;
-  const Triple before = scan_threads({(int64_t)max(fresh - old, 0), max(p1 - p0, 0), max(p0 - p1, 0)}, total, lds_sum);
-  row_first[t] = clipped(before.rows), grow_first[t] = before.grow, shrink_first[t] = before.shrink, old_len[t] = old;
-  if (t < a.n_seqs) cu[t] = clipped(before.rows);
-  if (t == 0) cu[a.n_seqs] = clipped(total.rows);
-  __syncthreads();
-  const int last = a.n_seqs - 1;
-  for (int i = t; i < total.grow; i += kPoolThreads) {
-    const int b = find_seq(grow_first, 0, last, i);
-    a.table[(int64_t)b * a.table_stride + a.pages(old_len[b]) + (i - grow_first[b])] = taken_page(a, st, i);
+  Triple mine[PER], sum{0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = t * PER + i;
+    int old = 0, fresh = 0;
+    if (b < a.n_seqs) old = max(len[b], 0), fresh = max(new_len[b], 0);
+    if constexpr (PER == 1) lds_len[b] = make_int2(old, fresh);
+    const int p0 = a.pages(old), p1 = a.pages(fresh);
+    mine[i] = {(int64_t)max(fresh - old, 0), max(p1 - p0, 0), max(p0 - p1, 0)};
+    sum.rows += mine[i].rows, sum.grow += mine[i].grow, sum.shrink += mine[i].shrink;
   }
-  if (positions || slots) {
-    const int n = (int)min((int64_t)rows, total.rows);
-    for (int i = t; i < n; i += kPoolThreads) {
-      const int b = find_seq(row_first, 0, last, i), pos = old_len[b] + (i - row_first[b]);
+  Triple total;
+  Triple before = scan_threads(sum, total, lds_sum);
+  const bool several = gridDim.x > 1 && (what & kGive);   // the first workgroup gives, the others fill
+  const bool gives = (what & kGive) && blockIdx.x == 0, fills = (what & kFill) && !(several && blockIdx.x == 0);
+  const int place = several ? (int)blockIdx.x - 1 : (int)blockIdx.x, share = several ? (int)gridDim.x - 1 : (int)gridDim.x;
+  const bool first_fill = fills && place == 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = t * PER + i;
+    row_first[b] = clipped(before.rows), grow_first[b] = before.grow, shrink_first[b] = before.shrink;
+    if (first_fill && b < a.n_seqs) cu[b] = clipped(before.rows);
+    before.rows += mine[i].rows, before.grow += mine[i].grow, before.shrink += mine[i].shrink;
+  }
+  if (first_fill && t == 0) cu[a.n_seqs] = clipped(total.rows);
+  __syncthreads();
+  const auto old_of = [&](int b) { return PER == 1 ? lds_len[b].x : max(len[b], 0); };
+  const auto new_of = [&](int b) { return PER == 1 ? lds_len[b].y : max(new_len[b], 0); };
+  const int last = a.n_seqs - 1;
+  const int n_rows = fills && (positions || slots) ? (int)min((int64_t)rows, total.rows) : 0, n_grow = fills ? total.grow : 0;
+  const int n_shrink = gives ? total.shrink : 0;
+  int given = 0;
+  // turn by turn, an entry and a row, and entries that are given back
+  const int64_t stride = (int64_t)share * kPoolThreads;
+  int64_t base = fills ? (int64_t)place * kPoolThreads : 0;
+  for (int64_t back = 0; base < max(n_rows, n_grow) || back < n_shrink; base += stride, back += 4 * kPoolThreads) {
+    const int64_t i = base + t;
+    int fresh_page = -1, page = -1, pos = 0;
+    int32_t *entry_at = nullptr;
+    if (i < n_grow) {
+      const int b = find_seq(grow_first, 0, last, (int)i);
+      entry_at = a.table + (int64_t)b * a.table_stride + a.pages(old_of(b)) + ((int)i - grow_first[b]);
+      fresh_page = taken_page(a, st, (int)i);
+    }
+    if (i < n_rows) {
+      const int b = find_seq(row_first, 0, last, (int)i), old = old_of(b), had = a.pages(old);
+      pos = old + ((int)i - row_first[b]);
+      const int entry = pos >> a.page_shift;
+      if (slots && entry < had) page = a.table[(int64_t)b * a.table_stride + entry];
+      else if (slots && entry < a.pages_per_seq) page = taken_page(a, st, grow_first[b] + entry - had);
+    }
+    if (back < n_shrink) give_pages(a, st, shrink_first, back, n_shrink, new_of, given, lds_given);
+    if (entry_at) *entry_at = fresh_page;
+    if (i < n_rows) {
       if (positions) positions[i] = pos;
-      if (slots) {
-        const int entry = pos >> a.page_shift, had = a.pages(old_len[b]);
-        int page = -1;
-        if (entry < had) page = a.table[(int64_t)b * a.table_stride + entry];
-        else if (entry < a.pages_per_seq) page = taken_page(a, st, grow_first[b] + entry - had);
-        slots[i] = slot_of(a, page, pos);
-      }
+      if (slots) slots[i] = slot_of(a, page, pos);
     }
   }
-  const int given = give_back(a, st, shrink_first, total.shrink, lds_votes);
-  if (t == 0) leave_state(a, st, total.grow, given, state_out);
+  if (gives && t == 0) leave_state(a, st, total.grow, given, state_out);
 }
 
-// The same in two launches.  First one workgroup adds up all sequences, leaves the sums in `cu` and the workspace, gives pages back
+// More sequences, in two launches.  First one workgroup adds up all sequences, leaves the sums in `cu` and the workspace, gives pages back
 // and writes the new state.
 struct PoolPlan {
   int32_t state[4];                                      // as it was
@@ -165,7 +219,7 @@ struct PoolPlan {
 };
 __global__ __launch_bounds__(kPoolThreads) void pool_plan_kernel(const int32_t *state, PoolArgs a, int32_t *state_out, int32_t *cu, PoolPlan *plan) {
   __shared__ Triple lds_sum[kPoolWaves];
-  __shared__ int lds_votes[kPoolWaves];
+  __shared__ int lds_given[kPoolWaves];
   const int t = threadIdx.x;
   const PoolState st(state, a.n_pages);
   int32_t *grow_first = plan->grow_first(), *shrink_first = grow_first + a.n_seqs;
@@ -183,10 +237,13 @@ __global__ __launch_bounds__(kPoolThreads) void pool_plan_kernel(const int32_t *
       shrink_first[b] = sum.shrink + before.shrink;
     }
     sum.rows += total.rows, sum.grow += total.grow, sum.shrink += total.shrink;
+    __syncthreads();                                     // (the sums' place is used again)
   }
   __threadfence_block();
   __syncthreads();
-  const int given = give_back(a, st, shrink_first, sum.shrink, lds_votes);
+  int given = 0;
+  for (int64_t back = 0; back < sum.shrink; back += 4 * kPoolThreads)
+    give_pages(a, st, shrink_first, back, sum.shrink, [&](int b) { return max(a.new_len[b], 0); }, given, lds_given);
   if (t == 0) {
     cu[a.n_seqs] = clipped(sum.rows);
     *reinterpret_cast<int4 *>(plan->state) = make_int4(st.head, st.count, 0, 0);
@@ -198,22 +255,9 @@ __global__ __launch_bounds__(kPoolThreads) void pool_plan_kernel(const int32_t *
 // Then many fill tables, positions and places.  A wavefront takes 64 consecutive rows (or entries) at a time: their sequences lie between
 // the first one's and the last one's, which all lanes look for together.
 __device__ __forceinline__ int find_seq_wave(const int *first, int n_seqs, int x, int total) {
-  const int lane = threadIdx.x & 63;
   const int x0 = __builtin_amdgcn_readfirstlane(x), x1 = min(x0 + 63, total - 1);
-  int lo[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int want = k ? x1 : x0;
-    int from = k ? lo[0] : 0, len = n_seqs - from;         // the answer is in [from, from + len)
-    while (len > 1) {
-      const int step = (len + 63) / 64, i = from + lane * step;
-      const int hits = __popcll(__ballot(lane * step < len && first[min(i, n_seqs - 1)] <= want));
-      from += (hits - 1) * step;
-      len = min(step, n_seqs - from);
-    }
-    lo[k] = from;
-  }
-  return find_seq(first, lo[0], lo[1], min(x, x1));
+  const int lo = find_seq_all(first, 0, n_seqs, x0);
+  return find_seq(first, lo, find_seq_all(first, lo, n_seqs, x1), min(x, x1));
 }
 __global__ __launch_bounds__(256) void pool_fill_kernel(PoolArgs a, const int32_t *cu, PoolPlan *plan, int rows, int row_blocks, int32_t *positions,
                                                         int64_t *slots) {
@@ -244,7 +288,7 @@ __global__ __launch_bounds__(256) void pool_fill_kernel(PoolArgs a, const int32_
   }
 }
 
-static bool in_one(int n_seqs, int rows) { return n_seqs <= kOneSeqs && rows <= kOneRows; }
+constexpr int kLdsSeqs = 4 * kPoolThreads;               // sequences whose sums a workgroup keeps
 
 }  // namespace et
 
@@ -252,8 +296,8 @@ using namespace et;
 
 extern "C" {
 
-size_t et_kv_resize_workspace_bytes(int32_t n_seqs, int32_t rows) {
-  if (n_seqs < 1 || rows < 0 || in_one(n_seqs, rows)) return 0;
+size_t et_kv_resize_workspace_bytes(int32_t n_seqs) {
+  if (n_seqs <= kLdsSeqs) return 0;
   return sizeof(PoolPlan) + 2 * sizeof(int32_t) * (size_t)n_seqs;
 }
 
@@ -275,7 +319,7 @@ int et_kv_resize(const et_kv_pool *pool, const int32_t *state_dev, int32_t *stat
   ET_REQUIRE(cu_rows_dev != nullptr, "cu_rows_dev is NULL");
   ET_REQUIRE(n_seqs == 0 || (page_table_dev && kv_len_dev && new_len_dev), "page_table_dev, kv_len_dev or new_len_dev is NULL");
   ET_REQUIRE((uintptr_t)slots_dev % 8 == 0, "slots_dev is not aligned to 8 bytes");
-  const size_t need = et_kv_resize_workspace_bytes(n_seqs, rows);
+  const size_t need = et_kv_resize_workspace_bytes(n_seqs);
   if (need) {
     ET_REQUIRE(workspace_dev != nullptr && (uintptr_t)workspace_dev % 16 == 0, "workspace_dev is NULL or not aligned to 16 bytes");
     if (workspace_bytes < need) {
@@ -286,9 +330,18 @@ int et_kv_resize(const et_kv_pool *pool, const int32_t *state_dev, int32_t *stat
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const PoolArgs a{pool->ring_dev, page_table_dev, kv_len_dev, new_len_dev, pool->n_pages, __builtin_ctz(page), table_stride, pages_per_seq, n_seqs};
   if (!need) {
-    pool_step_kernel<<<1, kPoolThreads, 0, stream>>>(state_dev, kv_len_dev, new_len_dev, rows, a, state_out_dev, cu_rows_dev, positions_dev, slots_dev);
-    ET_LAUNCH_CHECK();
-    return ET_OK;
+    // one workgroup for a decoding step; more for rows by the thousand
+    const int fillers = (int)std::min<int64_t>(255, ((int64_t)std::max(rows, n_seqs) + 2 * kPoolThreads - 1) / (2 * kPoolThreads));
+    const bool one = fillers <= 1, apart = !one && state_out_dev == state_dev;
+    auto launch = [&](int blocks, int what) {
+      (n_seqs <= kPoolThreads ? pool_resize_kernel<1> : pool_resize_kernel<4>)<<<blocks, kPoolThreads, 0, stream>>>(
+          state_dev, kv_len_dev, new_len_dev, rows, what, a, state_out_dev, cu_rows_dev, positions_dev, slots_dev);
+      ET_LAUNCH_CHECK();
+      return ET_OK;
+    };
+    int rc;
+    if ((rc = launch(one ? 1 : apart ? fillers : fillers + 1, apart ? kFill : kFill | kGive)) || !apart) return rc;
+    return launch(1, kGive);
   }
   PoolPlan *plan = static_cast<PoolPlan *>(workspace_dev);
   pool_plan_kernel<<<1, kPoolThreads, 0, stream>>>(state_dev, a, state_out_dev, cu_rows_dev, plan);

@@ -57,11 +57,11 @@ class World:
 
 @pytest.mark.parametrize("n_seqs,wide,page,pages,most", [
     (1, 1, 16, 1, 16), (1, 9, 16, 8, 150), (5, 6, 32, 40, 200), (64, 20, 16, 500, 330), (65, 3, 64, 150, 200), (256, 12, 64, 2000, 800),
-    (1024, 4, 16, 2500, 64), (1025, 4, 16, 2500, 64), (3000, 3, 256, 5000, 800), (7, 700, 16, 4000, 11000), (2, 3000, 16, 5000, 48000),
+    (1024, 4, 16, 2500, 64), (1025, 4, 16, 2500, 64), (3000, 3, 256, 5000, 800), (4096, 3, 32, 7000, 100), (4097, 3, 32, 7000, 100), (9000, 2, 16, 9000, 40), (7, 700, 16, 4000, 11000), (2, 3000, 16, 5000, 48000),
 ])
 def test_steps_that_grow_shrink_and_end(n_seqs, wide, page, pages, most):
-    """Random steps with pages missing now and then, lengths past the table's end among them; both forms (up to 8192 rows and 1024
-    sequences, and beyond)."""
+    """Random steps with pages missing now and then, lengths past the table's end among them; all forms (up to 1024, up to 4096 and more
+    sequences, a few rows and thousands)."""
     rng = np.random.default_rng(n_seqs + wide + page)
     lens = [int(x) for x in rng.integers(0, most + 1, n_seqs) * (rng.random(n_seqs) < 0.5)]
     w = World(rng, n_seqs, wide, pages, page, lens, pad=int(rng.integers(0, 4)))
@@ -85,7 +85,7 @@ def test_no_sequences_and_empty_ones():
 
 def test_fewer_rows_than_new_tokens():
     """positions and slots end where the caller says; pages are given all the same."""
-    for n, rows in ((4, 0), (4, 7), (4, 100), (1100, 50)):
+    for n, rows in ((4, 0), (4, 7), (4, 100), (1100, 50), (4200, 50)):
         rng = np.random.default_rng(rows)
         w = World(rng, n, 8, n * 4, 16, [int(x) for x in rng.integers(0, 30, n)])
         w.step([x + int(rng.integers(0, 60)) for x in w.lens], rows=rows)
@@ -121,7 +121,7 @@ def test_states_that_are_no_states():
         w.step([0, 0, 0, 0])
 
 
-@pytest.mark.parametrize("n,most", [(6, 100), (6, 4000), (1100, 40)])
+@pytest.mark.parametrize("n,most", [(6, 100), (6, 4000), (1100, 40), (4200, 20)])
 def test_a_call_is_taken_back_by_the_old_state(n, most):
     """With its state elsewhere, a call (one that lacks pages) changes nothing that the old state and lengths reach: another one
     follows as if it had not been."""
@@ -148,7 +148,7 @@ def test_positions_or_slots_alone():
     import ctypes as C
     from paper_2605_30010_amd import binding as B
     lib = et.load_library()
-    for n in (3, 1100):
+    for n in (3, 1100, 4200):
         for keep in ((True, False), (False, True), (False, False)):
             w = World(np.random.default_rng(7), n, 4, 4 * n, 16, [3] * n)
             new = [20] * n
@@ -156,7 +156,7 @@ def test_positions_or_slots_alone():
             old, want, cu_dev = ints(w.lens), ints(new), torch.zeros(n + 1, dtype=torch.int32, device="cuda:0")
             p = torch.zeros(len(positions), dtype=torch.int32, device="cuda:0")
             s = torch.zeros(len(positions), dtype=torch.int64, device="cuda:0")
-            ws = torch.zeros(1 << 16, dtype=torch.uint8, device="cuda:0")
+            ws = torch.zeros(1 << 17, dtype=torch.uint8, device="cuda:0")
             rc = lib.et_kv_resize(C.byref(w.pool._pool), w.pool.state.data_ptr(), w.pool.state.data_ptr(), w.dev_table.data_ptr(), 4, 4, old.data_ptr(),
                                   want.data_ptr(), n, len(positions), cu_dev.data_ptr(), p.data_ptr() if keep[0] else None,
                                   s.data_ptr() if keep[1] else None, ws.data_ptr(), ws.numel(), B._raw_stream(0))
@@ -165,7 +165,7 @@ def test_positions_or_slots_alone():
             assert p.tolist() == (positions if keep[0] else [0] * len(positions)) and s.tolist() == (slots if keep[1] else [0] * len(slots))
 
 
-@pytest.mark.parametrize("n", [5, 1100])
+@pytest.mark.parametrize("n", [5, 1100, 4200])
 def test_a_captured_step_takes_a_page_when_it_needs_one(n):
     """Replays of one graph, in which the lengths are counted up too, against the definition; eager work between them."""
     rng = np.random.default_rng(8)

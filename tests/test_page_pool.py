@@ -39,7 +39,7 @@ def call(pool=None, state=FAKE, state_out=FAKE, table=FAKE, stride=4, pages=4, o
                                  dict(state=FAKE + 8), dict(state_out=None), dict(state_out=FAKE + 4), dict(table=None), dict(old=None), dict(new=None),
                                  dict(n=-1), dict(n=2 ** 20 + 1), dict(stride=3), dict(pages=0), dict(pages=1 << 27, stride=1 << 27),
                                  dict(n=1 << 16, pages=1 << 15, stride=1 << 15), dict(rows=-1), dict(cu=None), dict(slots=FAKE + 4),
-                                 dict(n=2000, ws=None), dict(n=2000, ws=FAKE + 8)])
+                                 dict(n=5000, ws=None), dict(n=5000, ws=FAKE + 8)])
 def test_refused_calls(bad):
     assert call(**bad) == -1 and et.et_last_error()
 
@@ -48,10 +48,9 @@ def test_null_pool_and_workspace():
     lib = et.load_library()
     assert lib.et_kv_resize(None, FAKE, FAKE, FAKE, 4, 4, FAKE, FAKE, 3, 5, FAKE, FAKE, FAKE, FAKE, 1 << 40, None) == -1
     need = lib.et_kv_resize_workspace_bytes
-    assert need(1, 0) == need(1024, 8192) == need(0, 10 ** 6) == need(-1, 5) == need(5, -1) == 0
-    assert need(1025, 0) > 0 and need(3, 8193) > 0 and need(2 ** 20, 2 ** 31 - 1) < 1 << 24
-    assert call(n=2000, ws_bytes=need(2000, 5) - 1) == -2 and "workspace" in et.et_last_error()
-    assert call(n=3, rows=8193, ws_bytes=0) == -2
+    assert need(-1) == need(0) == need(1) == need(4096) == 0
+    assert 0 < need(4097) < need(2 ** 20) < 1 << 24
+    assert call(n=5000, ws_bytes=need(5000) - 1) == -2 and "workspace" in et.et_last_error()
 
 
 def test_refused_slots():
