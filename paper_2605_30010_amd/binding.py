@@ -1,5 +1,6 @@
-"""ctypes binding of include/earlytom.h.  Argument marshalling only."""
+"""ctypes binding of include/earlytom.h.  Argument marshalling only (csrc/calls.cpp makes the usual calls of a decoding step)."""
 import ctypes as C
+import importlib
 import math
 import os
 
@@ -9,6 +10,7 @@ import torch
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libearlytom.so")
 _lib = None
+_calls = None
 
 ET_OK = 0
 ET_K_COUNT = 15
@@ -93,13 +95,15 @@ def library_path():
 
 
 def load_library():
-    """Load libearlytom.so; raises (never falls back) when it has not been built."""
-    global _lib
+    """Load libearlytom.so and the native part of this binding; raises (never falls back) when they have not been built."""
+    global _lib, _calls
     if _lib is not None:
         return _lib
     if not os.path.exists(_LIB_PATH):
         raise ImportError("libearlytom.so is not built: run `python -c 'import __graft_entry__ as g; "
                           "g.build()'` (or python paper_2605_30010_amd/build.py) first")
+    calls = importlib.import_module(__package__ + "._calls")
+    calls.bind(_LIB_PATH)
     lib = C.CDLL(_LIB_PATH)
     i32, i64, f32, vp, sz = C.c_int32, C.c_int64, C.c_float, C.c_void_p, C.c_size_t
     sig = {
@@ -155,7 +159,7 @@ def load_library():
         fn = getattr(lib, name)
         fn.restype = res
         fn.argtypes = args
-    _lib = lib
+    _lib, _calls = lib, calls
     return lib
 
 
@@ -602,6 +606,11 @@ def et_kv_page_bytes(page_size, n_kv_heads, head_dim, fmt):
 class _OnDevice:
     """Something whose calls run on its own device (`device`), on that device's current stream or one that is given."""
 
+    _calls = None                                        # csrc/calls.cpp, with what it takes: the descriptor's address, the device's index
+
+    def _number(self):
+        return -1 if self.device.index is None else self.device.index
+
     def _here(self, stream):
         """The stream to launch on, if its device is the current one and no other stream is asked for."""
         if stream is None and _current_device() == self.device.index:
@@ -615,6 +624,13 @@ class _OnDevice:
         if stream.device != self.device:
             raise ValueError("the stream is on %s, not on %s" % (stream.device, self.device))
         return torch.cuda.stream(stream)
+
+
+def _made(result):
+    """What csrc/calls.cpp returned: results, or an entry point's error code."""
+    if type(result) is int:
+        _check(result)
+    return result
 
 
 class KVCache(_OnDevice):
@@ -641,6 +657,7 @@ class KVCache(_OnDevice):
         self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = int(n_pages), int(page_size), int(n_kv_heads), int(head_dim)
         self._cache = _KvCache(data.data_ptr(), self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, _KV_FORMATS[fmt])
         self._lib, self._width, self._scale = load_library(), self.n_kv_heads * self.head_dim, 1.0 / math.sqrt(self.head_dim)
+        self._calls, self._at, self._index = _calls, C.addressof(self._cache), self._number()
 
     def append(self, k, v, page_table, kv_len, cu_rows=None, stream=None):
         """Stores rows k, v (bf16 [rows, n_kv_heads * head_dim] or [rows, n_kv_heads, head_dim], rows may be strided) as the last
@@ -649,6 +666,10 @@ class KVCache(_OnDevice):
         if s is None:
             with self._elsewhere(stream):
                 return self.append(k, v, page_table, kv_len, cu_rows)
+        if self._calls is not None:
+            code = self._calls.append(self._at, self._index, k, v, page_table, kv_len, cu_rows, s)
+            if code is not None:
+                return _check(code) if code else None
         k, rows, _, k_stride = self._rows(k, "k", self._width)
         v, v_rows, _, v_stride = self._rows(v, "v", self._width)
         if v_rows != rows:
@@ -664,6 +685,10 @@ class KVCache(_OnDevice):
         if s is None:
             with self._elsewhere(stream):
                 return self.append_at(k, v, slots)
+        if self._calls is not None:
+            code = self._calls.append_at(self._at, self._index, k, v, slots, s)
+            if code is not None:
+                return _check(code) if code else None
         k, rows, _, k_stride = self._rows(k, "k", self._width)
         v, v_rows, _, v_stride = self._rows(v, "v", self._width)
         if v_rows != rows:
@@ -682,6 +707,10 @@ class KVCache(_OnDevice):
         if s is None:
             with self._elsewhere(stream):
                 return self.read(page_table, kv_len, cu_rows, rows, out)
+        if self._calls is not None and out is None:
+            made = self._calls.read(self._at, self._index, page_table, kv_len, cu_rows, rows, s)
+            if made is not None:
+                return _made(made)
         seqs = self._seqs(page_table, kv_len)
         cu = None if cu_rows is None else self._cu(cu_rows, kv_len)
         if out is None:
@@ -708,6 +737,10 @@ class KVCache(_OnDevice):
         if s is None:
             with self._elsewhere(stream):
                 return self.attend(q, page_table, kv_len, max_len, window, scale, out)
+        if self._calls is not None and out is None:
+            made = self._calls.attend(self._at, self._index, q, page_table, kv_len, max_len, window, self._scale if scale is None else scale, s)
+            if made is not None:
+                return _made(made)
         q, n, width, q_stride = self._rows(q, "q", 0)
         seqs, lib = self._seqs(page_table, kv_len), self._lib
         if n != seqs.n_seqs:
@@ -778,6 +811,7 @@ class PagePool(_OnDevice):
         self.ring, self.state, self.device = ring, state, ring.device
         self.n_pages, self.page_size, self._lib = int(n_pages), int(page_size), load_library()
         self._pool = _KvPool(ring.data_ptr(), self.n_pages, self.page_size)
+        self._calls, self._at, self._index = _calls, C.addressof(self._pool), self._number()
 
     def resize(self, page_table, kv_len, new_len, rows, state_out=None, out=None, stream=None):
         """Takes every sequence from kv_len to new_len tokens (int32 [n_seqs] each): its row of page_table (int32 [n_seqs, pages], rows may
@@ -789,6 +823,11 @@ class PagePool(_OnDevice):
         if s is None:
             with self._elsewhere(stream):
                 return self.resize(page_table, kv_len, new_len, rows, state_out, out)
+        if self._calls is not None and out is None:
+            made = self._calls.resize(self._at, self._index, self.state, self.state if state_out is None else state_out, page_table, kv_len, new_len,
+                                      rows, s)
+            if made is not None:
+                return _made(made)
         shape, strides = self._ints(page_table, "page_table").shape, page_table.stride()
         if len(shape) != 2 or shape[1] < 1 or (strides[1] != 1 and shape[1] > 1):
             raise ValueError("page_table must be [n_seqs, pages] with contiguous rows")
@@ -868,6 +907,7 @@ class Rotary(_OnDevice):
         self.steps = torch.from_numpy(steps.view(np.int64)).to(device)
         self.device, self._lib = self.steps.device, load_library()
         self._rotary = _Rotary(self.steps.data_ptr(), self.head_dim, self.rot_dim, _ROTARY_LAYOUTS[layout], self.amplitude)
+        self._calls, self._at, self._index = _calls, C.addressof(self._rotary), self._number()
 
     def apply(self, q, k, positions, out=None, transpose=False, stream=None):
         """Turns q and k, bf16 [rows, heads * head_dim] or [rows, heads, head_dim] (rows may be strided; k may be None), by positions int32
@@ -877,6 +917,10 @@ class Rotary(_OnDevice):
         if s is None:
             with self._elsewhere(stream):
                 return self.apply(q, k, positions, out, transpose)
+        if self._calls is not None and out is None:
+            made = self._calls.rotate(self._at, self._index, q, k, positions, bool(transpose), s)
+            if made is not None:
+                return _made(made)
         if not (isinstance(positions, torch.Tensor) and positions.dtype is torch.int32 and positions.device == self.device):
             raise TypeError("positions must be an int32 tensor on %s" % self.device)
         rows = positions.shape

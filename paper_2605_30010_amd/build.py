@@ -1,7 +1,8 @@
-"""Builds libearlytom.so (HIP, gfx950 only) in-tree with hipcc."""
+"""Builds libearlytom.so (HIP, gfx950 only) in-tree with hipcc, and the binding's native part with g++."""
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -9,6 +10,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libearlytom.so")
 OBJ_DIR = os.path.join(PKG, "_build")
+CALLS = os.path.join(PKG, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -31,12 +33,29 @@ def _compile(src):
     return src, obj, r
 
 
+def _build_calls():
+    """csrc/calls.cpp as a Python extension beside the library (host code against torch's headers)."""
+    import torch
+    from torch.utils import cpp_extension
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"]]
+    for path in cpp_extension.include_paths():
+        cmd += ["-isystem", path]
+    cmd += [os.path.join(CSRC, "calls.cpp"), "-o", CALLS]
+    for path in cpp_extension.library_paths():
+        cmd += ["-L", path]
+    return subprocess.run(cmd + ["-lc10", "-ltorch_cpu", "-ltorch_python", "-ldl"], capture_output=True, text=True)
+
+
 def build_library(verbose=True):
-    """Compile every csrc/*.hip for gfx950 and link libearlytom.so.  Always recompiles."""
+    """Compile every csrc/*.hip for gfx950 and link libearlytom.so; build the binding's native part.  Always recompiles."""
     os.makedirs(OBJ_DIR, exist_ok=True)
     srcs = sources()
-    with ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
+    with ThreadPoolExecutor(max_workers=min(8, len(srcs) + 1)) as ex:
+        calls = ex.submit(_build_calls)
         results = list(ex.map(_compile, srcs))
+    if calls.result().returncode != 0:
+        raise RuntimeError("g++ failed on calls.cpp:\n%s" % calls.result().stderr)
     objs = []
     for src, obj, r in results:
         noise = "unknown target feature"     # hipcc's host pass does not know -packed-fp32-ops
