@@ -917,8 +917,9 @@ class Rotary(_OnDevice):
         if s is None:
             with self._elsewhere(stream):
                 return self.apply(q, k, positions, out, transpose)
-        if self._calls is not None and out is None:
-            made = self._calls.rotate(self._at, self._index, q, k, positions, bool(transpose), s)
+        if self._calls is not None:
+            q_out, k_out = (None, None) if out is None else out
+            made = self._calls.rotate(self._at, self._index, q, k, positions, q_out, k_out, bool(transpose), s)
             if made is not None:
                 return _made(made)
         if not (isinstance(positions, torch.Tensor) and positions.dtype is torch.int32 and positions.device == self.device):

@@ -213,28 +213,45 @@ CALL(resize) {
   END_HANDLE_TH_ERRORS
 }
 
-// (rotary, device, q, k or None, positions, transpose, stream) -> (q, k)
+// (rotary, device, q, k or None, positions, q_out or None, k_out or None, transpose, stream) -> (q, k)
 CALL(rotate) {
   HANDLE_TH_ERRORS
   const auto *rotary = at_address<et_rotary>(arg[0]);
   const long device = PyLong_AsLong(arg[1]);
-  const int64_t d = rotary->head_dim;
-  const bool keys = arg[3] != Py_None;
-  const Rows q(arg[2], device, d), k(keys ? arg[3] : arg[2], device, d);
-  if (!q.t || !k.t || q.n != k.n || q.n > INT32_MAX || q.heads > 65536 || k.heads > 65536) Py_RETURN_NONE;
-  const at::Tensor *positions = ints(arg[4], device, q.n);
+  PyObject *out[2] = {nullptr, nullptr};                 // (borrowed where given)
+  at::Tensor made_here[2];
+  et_rotary_rows rows[2]{};
+  int64_t n = 0;
+  for (int i = 0; i < 2; ++i) {
+    if (i && arg[3] == Py_None) break;
+    const Rows x(arg[2 + i], device, rotary->head_dim);
+    if (!x.t || x.heads > 65536 || x.n > INT32_MAX || (i && x.n != n)) Py_RETURN_NONE;
+    n = x.n;
+    rows[i] = {x.data(), x.stride, nullptr, x.heads * rotary->head_dim, (int32_t)x.heads};
+    if (arg[5 + i] != Py_None) {
+      const Rows to(arg[5 + i], device, rotary->head_dim);
+      if (!to.t || to.n != n || to.heads != x.heads) Py_RETURN_NONE;
+      out[i] = arg[5 + i];
+      rows[i].out_dev = to.data();
+      rows[i].out_stride = to.stride;
+    } else {
+      made_here[i] = fresh(x.t->sizes(), at::kBFloat16, device);
+      rows[i].out_dev = static_cast<uint16_t *>(made_here[i].data_ptr());
+    }
+  }
+  const at::Tensor *positions = ints(arg[4], device, n);
   if (!positions) Py_RETURN_NONE;
-  const at::Tensor q_out = fresh(q.t->sizes(), at::kBFloat16, device);
-  at::Tensor k_out;
-  if (keys) k_out = fresh(k.t->sizes(), at::kBFloat16, device);
-  const et_rotary_rows q_rows{q.data(), q.stride, static_cast<uint16_t *>(q_out.data_ptr()), q.heads * d, (int32_t)q.heads};
-  et_rotary_rows k_rows{};
-  if (keys) k_rows = {k.data(), k.stride, static_cast<uint16_t *>(k_out.data_ptr()), k.heads * d, (int32_t)k.heads};
   const int rc = unlocked([&] {
-    return lib.rotary(rotary, static_cast<const int32_t *>(positions->data_ptr()), (int32_t)q.n, &q_rows, keys ? &k_rows : nullptr,
-                      arg[5] == Py_True, stream_of(arg[6]));
+    return lib.rotary(rotary, static_cast<const int32_t *>(positions->data_ptr()), (int32_t)n, &rows[0], arg[3] == Py_None ? nullptr : &rows[1],
+                      arg[7] == Py_True, stream_of(arg[8]));
   });
-  return keys ? made(rc, q_out, k_out) : rc ? done(rc) : Py_BuildValue("(NO)", THPVariable_Wrap(q_out), Py_None);
+  if (rc) return done(rc);
+  for (int i = 0; i < 2; ++i) {
+    if (out[i]) Py_INCREF(out[i]);
+    else if (made_here[i].defined()) out[i] = THPVariable_Wrap(made_here[i]);
+    else Py_INCREF(out[i] = Py_None);
+  }
+  return Py_BuildValue("(NN)", out[0], out[1]);
   END_HANDLE_TH_ERRORS
 }
 

@@ -79,23 +79,24 @@ __device__ __forceinline__ int find_seq_all(const int *first, int from, int n_se
   }
   return from;
 }
-// Gives pages behind sequences' ends back: of all `total` entries the workgroup takes 4096 from `back` on, a wavefront 256 neighbours (their
-// sequences lie between the first one's and the last one's).  Those that are pages go behind the ring's `count` free ones and the
+// Gives pages behind sequences' ends back: of all `total` entries the workgroup takes up to 4096 from `back` on, a wavefront up to 256
+// neighbours (their sequences lie between the first one's and the last one's).  Those that are pages go behind the ring's `count` free ones and the
 // `given` before them, in order.
 template <typename NewLength>
 __device__ __forceinline__ void give_pages(const PoolArgs &a, PoolState st, const int *shrink_first, int64_t back, int total, NewLength new_of,
                                            int &given, int (&lds)[kPoolWaves]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, room = a.n_pages - st.count;
-  const int64_t k0 = back + wave * 256;
+  const int each = 64 * (int)min((total - back + kPoolThreads - 1) / kPoolThreads, (int64_t)4);      // entries of a wavefront
+  const int64_t k0 = back + wave * each;
   int page[4], mine = 0;
   uint64_t votes[4] = {};
   if (k0 < total) {
-    const int lo = find_seq_all(shrink_first, 0, a.n_seqs, (int)k0), hi = find_seq_all(shrink_first, lo, a.n_seqs, (int)min(k0 + 255, total - 1ll));
+    const int lo = find_seq_all(shrink_first, 0, a.n_seqs, (int)k0), hi = find_seq_all(shrink_first, lo, a.n_seqs, (int)min(k0 + each - 1, total - 1ll));
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int64_t k = k0 + u * 64 + lane;
       page[u] = -1;
-      if (k < total) {
+      if (k < min(k0 + each, (int64_t)total)) {
         const int b = find_seq(shrink_first, lo, hi, (int)k);
         page[u] = a.table[(int64_t)b * a.table_stride + a.pages(new_of(b)) + ((int)k - shrink_first[b])];
       }
