@@ -191,19 +191,20 @@ __device__ __forceinline__ uint32_t mx_encode8(u32x4 x, uint32_t exponent) {
 // the way to a place is a chain of four loads, so rows share it when there are many.  What is read or written once in long
 // streams (new rows, unquantised cells, rows read back) goes past the caches: 391 MB of e4m3 codes read back 265 -> 254 us, 130 000
 // rows of 4 heads of 80 73 -> 65, 134 MB of bfloat16 rows stored 110 -> 101; codes and the cells of a read do not gain by it.
+// SLOTS: the rows' places are given, in the place of `cu`.
 constexpr int kBatch = 4;
-template <int HD, int FMT, bool STORE>
+template <int HD, int FMT, bool STORE, bool SLOTS>
 __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const int32_t *len, const int32_t *table, int n_seqs, int rows,
                                                       int per_block, int table_stride, int pages_per_seq, int page_shift, KvPages c,
-                                                      uint16_t *k, int64_t k_stride, uint16_t *v, int64_t v_stride,
-                                                      const int64_t *slots) {
+                                                      uint16_t *k, int64_t k_stride, uint16_t *v, int64_t v_stride) {
   using Lay = KvLayout<HD, FMT>;
   constexpr int LANES = kv_lanes<HD>(), GROUPS = 256 / LANES;
   __shared__ int4 lds_place[64];                         // byte offset of the page (two words), token of the page, 0 / 1 / 2
   const int first = blockIdx.x * per_block, count = min(per_block, rows - first);
   if (threadIdx.x < 64) {
-    const KvPlace p = slots ? kv_slot(slots, first, count, c.n_pages, page_shift)
-                            : kv_place(cu, first, count, KvSeqs{table, len, table_stride, pages_per_seq, n_seqs}, c.n_pages, page_shift);
+    KvPlace p;
+    if constexpr (SLOTS) p = kv_slot(reinterpret_cast<const int64_t *>(cu), first, count, c.n_pages, page_shift);
+    else p = kv_place(cu, first, count, KvSeqs{table, len, table_stride, pages_per_seq, n_seqs}, c.n_pages, page_shift);
     const int64_t page = max(p.page, 0) * c.page_bytes;
     lds_place[threadIdx.x] = make_int4((int)page, (int)(page >> 32), p.at, p.owned ? (p.page >= 0 ? 2 : 1) : 0);
   }
@@ -230,9 +231,12 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const i
       char *page = c.data + (int64_t)((uint64_t)(uint32_t)place.y << 32 | (uint32_t)place.x);
       const uint32_t head = (uint32_t)h * head_bytes;
       cell[i] = page + (head + (value ? Lay::values(n) : 0) + place.z * Lay::kRow + sub * Lay::kEight);
-      const int block = min(sub / (kMxBlock / 8), Lay::kBlocks - 1);
-      const int scale = FMT != ET_KV_MXFP4 ? 2 * place.z : value ? block * n + place.z : place.z * Lay::kBlocks + block;
-      top_at[i] = page + (head + (value ? Lay::value_scale(n) : Lay::key_scale(n)) + scale);
+      if constexpr (FMT == ET_KV_MXFP4) {
+        const int block = min(sub / (kMxBlock / 8), Lay::kBlocks - 1);
+        top_at[i] = page + (head + (value ? Lay::value_scale(n) + block * n + place.z : Lay::key_scale(n) + place.z * Lay::kBlocks + block));
+      } else {
+        top_at[i] = page + (head + (value ? Lay::value_scale(n) : Lay::key_scale(n)) + place.z * 2);
+      }
       x[i] = u32x4{0, 0, 0, 0};
       codes[i] = make_uint2(0, 0);
       top[i] = 0;
@@ -350,9 +354,10 @@ static int launch_rows(const et_kv_cache &cache, const et_kv_seqs &seqs, const i
   const KvPages c = kv_pages(cache);
   const int per_block = rows_per_block(rows, cache);
   auto launch = [&](auto hd, auto fmt) {
-    kv_rows_kernel<hd.value, fmt.value, STORE><<<(rows + per_block - 1) / per_block, 256, 0, stream>>>(
-        cu, seqs.kv_len_dev, seqs.page_table_dev, seqs.n_seqs, rows, per_block, seqs.table_stride, seqs.pages_per_seq, c.page_shift, c,
-        k, k_stride, v, v_stride, slots);
+    (slots ? kv_rows_kernel<hd.value, fmt.value, STORE, STORE> : kv_rows_kernel<hd.value, fmt.value, STORE, false>)<<<
+        (rows + per_block - 1) / per_block, 256, 0, stream>>>(
+        slots ? reinterpret_cast<const int32_t *>(slots) : cu, seqs.kv_len_dev, seqs.page_table_dev, seqs.n_seqs, rows, per_block, seqs.table_stride, seqs.pages_per_seq, c.page_shift, c,
+        k, k_stride, v, v_stride);
     ET_LAUNCH_CHECK();
     return ET_OK;
   };

@@ -214,65 +214,6 @@ struct PagedMore {                                       // the kernel's argumen
   int n_pages;
   float scale_log2;
 };
-// The end of a workgroup's part: its wavefronts' results (accumulators, reference m and this lane's sum of query head r) together, and out,
-// or to where the parts are joined.  `factor`: what the values are multiplied with.
-template <int HD, int DPL, int BLOCKS>
-__device__ __forceinline__ void finish_part(const PagedMore &o, const Part &part, const f32x4 (&acc)[BLOCKS * DPL], float m, float sum, float factor,
-                                            int wave, int live, int64_t head, int64_t slot, float (&lds_o)[kWaves][HD / BLOCKS][16],
-                                            float2 (&lds_ml)[kWaves][16]) {
-  constexpr int BD = HD / BLOCKS;                         // dimensions that the wavefronts add up at a time
-  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, h = threadIdx.x & 15;
-  sum += __shfl_xor(sum, 16, 64);
-  sum += __shfl_xor(sum, 32, 64);
-  if (g == 0) lds_ml[wave][r] = make_float2(m, sum);
-  float top = -INFINITY, total = 0.f, f[kWaves];
-#pragma unroll
-  for (int blk = 0; blk < BLOCKS; ++blk) {
-    if (blk) __syncthreads();
-    if (r < live) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int d = (4 * g + e) * DPL;
-        if (d < BD)
-#pragma unroll
-          for (int j = 0; j < DPL; ++j) lds_o[wave][d + j][r] = acc[blk * DPL + j][e];
-      }
-    }
-    __syncthreads();
-    if (blk == 0) {
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds_ml[w][h].x);
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float2 ml = lds_ml[w][h];
-        f[w] = part_factor(ml, top);
-        total += f[w] * ml.y;
-      }
-    }
-    for (int d = (threadIdx.x >> 4) * 8; h < live && d < BD; d += 4 * kWaves * 8) {
-      float x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) x[e] = fmaf(f[w], lds_o[w][d + e][h], x[e]);
-      }
-      if (part.count == 1) {
-        const float inv = factor / total;
-        u32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = total == 0.f ? 0 : cvt_pk_bf16(x[2 * e] * inv, x[2 * e + 1] * inv);  // (0 times x could be NaN)
-        *reinterpret_cast<u32x4 *>(o.out + head * HD + blk * BD + d) = v;
-      } else {
-        float *to = o.part_o + slot * HD + blk * BD + d;
-        *reinterpret_cast<f32x4 *>(to) = f32x4{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<f32x4 *>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
-      }
-    }
-  }
-  if (part.count > 1 && threadIdx.x < live) o.part_ml[slot] = make_float2(top, total);
-}
-
 // A workgroup takes one part of a sequence's tokens for up to 16 query heads of one key-value head; its wavefronts take tiles of
 // 32 tokens in turn: logits S^T = K Q^T, weights against a running reference, O^T += V^T P^T, where the accumulators that hold S^T are,
 // exponentiated and rounded, operand B of the second product (which tokens a lane's eight places of the contraction stand for is free, and the
@@ -463,10 +404,58 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_kernel(const i
   }
 
   // the wavefronts' results together
+  sum += __shfl_xor(sum, 16, 64);
+  sum += __shfl_xor(sum, 32, 64);
+  if (g == 0) lds_ml[wave][r] = make_float2(m, sum);
   const int h = threadIdx.x & 15;
   const int64_t head = (int64_t)b * n_heads + (int64_t)kv * group + rt * 16 + h;
   const int64_t slot = (int64_t)item * n_heads + kv * group + rt * 16 + h;       // of a part that is one of several
-  finish_part<HD, V::DPL, V::BLOCKS>(o, part, acc, m, sum, value_factor<FMT>(), wave, live, head, slot, lds_o, lds_ml);
+  float top = -INFINITY, total = 0.f, f[kWaves];
+#pragma unroll
+  for (int blk = 0; blk < V::BLOCKS; ++blk) {
+    if (blk) __syncthreads();
+    if (r < live) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int d = (4 * g + e) * V::DPL;
+        if (d < BD)
+#pragma unroll
+          for (int j = 0; j < V::DPL; ++j) lds_o[wave][d + j][r] = acc[blk * V::DPL + j][e];
+      }
+    }
+    __syncthreads();
+    if (blk == 0) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds_ml[w][h].x);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float2 ml = lds_ml[w][h];
+        f[w] = part_factor(ml, top);
+        total += f[w] * ml.y;
+      }
+    }
+    for (int d = (threadIdx.x >> 4) * 8; h < live && d < BD; d += 4 * kWaves * 8) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) x[e] = fmaf(f[w], lds_o[w][d + e][h], x[e]);
+      }
+      if (part.count == 1) {
+        const float inv = value_factor<FMT>() / total;
+        u32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = total == 0.f ? 0 : cvt_pk_bf16(x[2 * e] * inv, x[2 * e + 1] * inv);  // (0 times x could be NaN)
+        *reinterpret_cast<u32x4 *>(o.out + head * HD + blk * BD + d) = v;
+      } else {
+        float *to = o.part_o + slot * HD + blk * BD + d;
+        *reinterpret_cast<f32x4 *>(to) = f32x4{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<f32x4 *>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
+      }
+    }
+  }
+  if (part.count > 1 && threadIdx.x < live) o.part_ml[slot] = make_float2(top, total);
 }
 
 // What one launch of the kernel takes.

@@ -1,4 +1,6 @@
 // Attention of one new token per sequence over a paged key-value cache in 4 bits.
+#include <algorithm>
+
 #include "paged_attention.h"
 
 namespace et {
@@ -77,12 +79,72 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
+// The end of a workgroup's part: its wavefronts' results (accumulators, reference m and this lane's sum of query head r) together, and out,
+// or to where the parts are joined.  `factor`: what the values are multiplied with.  WAVES: wavefronts of the workgroup, of which the first kWaves
+// have results.
+template <int HD, int DPL, int BLOCKS, int WAVES>
+__device__ __forceinline__ void finish_part(const PagedMore &o, const Part &part, const f32x4 (&acc)[BLOCKS * DPL], float m, float sum, float factor,
+                                            int wave, int live, int64_t head, int64_t slot, float (&lds_o)[kWaves][HD / BLOCKS][16],
+                                            float2 (&lds_ml)[kWaves][16]) {
+  constexpr int BD = HD / BLOCKS;                         // dimensions that the wavefronts add up at a time
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, h = threadIdx.x & 15;
+  sum += __shfl_xor(sum, 16, 64);
+  sum += __shfl_xor(sum, 32, 64);
+  if (g == 0 && (WAVES == kWaves || wave < kWaves)) lds_ml[wave][r] = make_float2(m, sum);
+  float top = -INFINITY, total = 0.f, f[kWaves];
+#pragma unroll
+  for (int blk = 0; blk < BLOCKS; ++blk) {
+    if (blk) __syncthreads();
+    if (r < live && (WAVES == kWaves || wave < kWaves)) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int d = (4 * g + e) * DPL;
+        if (d < BD)
+#pragma unroll
+          for (int j = 0; j < DPL; ++j) lds_o[wave][d + j][r] = acc[blk * DPL + j][e];
+      }
+    }
+    __syncthreads();
+    if (blk == 0) {
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds_ml[w][h].x);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float2 ml = lds_ml[w][h];
+        f[w] = part_factor(ml, top);
+        total += f[w] * ml.y;
+      }
+    }
+    for (int d = (threadIdx.x >> 4) * 8; h < live && d < BD; d += 4 * kWaves * 8) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) x[e] = fmaf(f[w], lds_o[w][d + e][h], x[e]);
+      }
+      if (part.count == 1) {
+        const float inv = factor / total;
+        u32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = total == 0.f ? 0 : cvt_pk_bf16(x[2 * e] * inv, x[2 * e + 1] * inv);  // (0 times x could be NaN)
+        *reinterpret_cast<u32x4 *>(o.out + head * HD + blk * BD + d) = v;
+      } else {
+        float *to = o.part_o + slot * HD + blk * BD + d;
+        *reinterpret_cast<f32x4 *>(to) = f32x4{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<f32x4 *>(to + 4) = f32x4{x[4], x[5], x[6], x[7]};
+      }
+    }
+  }
+  if (part.count > 1 && threadIdx.x < live) o.part_ml[slot] = make_float2(top, total);
+}
+
 // As paged_attention_kernel: a workgroup takes one part of a sequence's tokens for up to 16 query heads of one key-value head, its
 // wavefronts tiles of 32 tokens in turn, S^T = K Q^T and O^T += V^T P^T by matrix instructions on bfloat16 numbers, which codes and their power of two
 // are exactly; a weight is the sum of two of them.  A tile's registers are loaded again as soon as they have become operands, so the next
 // tile's keys come in during the softmax and the second product, its values during that and the next logits.
-template <int HD, bool ONE>
-__global__ __launch_bounds__(64 * kWaves, 2) void paged_mxfp4_kernel(const int32_t *len, const int32_t *table, int n_seqs, int share, int bound,
+template <int HD, bool ONE, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_t *len, const int32_t *table, int n_seqs, int share, int bound,
                                                                  int window, int units, int row_tiles, int page_shift, int table_stride,
                                                                  int group, PagedMore o) {
   using Lay = KvLayout<HD, ET_KV_MXFP4>;
@@ -123,7 +185,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_mxfp4_kernel(const int32
   float m = -INFINITY, sum = 0.f;                         // of query head r; sum: this lane's tokens only
 
   const int32_t *row = table + (int64_t)b * table_stride;
-  const int mine = (tiles - wave + kWaves - 1) / kWaves;  // tiles of this wavefront
+  const int mine = (tiles - wave + WAVES - 1) / WAVES;  // tiles of this wavefront
   int page_of = -1;                                       // lane i: page of the i-th group of 16 tokens of 32 tiles of the wavefront
   // (A group of 16 tokens without a page reads the first page's bytes, and its tokens do not count.)
   auto head_of = [&](int page) { return o.data + max(page, 0) * o.page_bytes + (int64_t)kv * Lay::head_bytes(ps); };
@@ -133,9 +195,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_mxfp4_kernel(const int32
   };
   Tile x;
   auto load_keys = [&](int n) {                         // of the wavefront's n-th tile
-    const int t = wave + n * kWaves;
+    const int t = wave + n * WAVES;
     if ((n & 31) == 0) {
-      const int pos = start + (t + (lane >> 1) * kWaves) * kTile + (lane & 1) * 16;
+      const int pos = start + (t + (lane >> 1) * WAVES) * kTile + (lane & 1) * 16;
       page_of = pos < end ? row[pos >> page_shift] : -1;
       if (page_of >= o.n_pages) page_of = -1;
     }
@@ -151,7 +213,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_mxfp4_kernel(const int32
   auto load_values = [&](int n, int blk) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int at = (start + (wave + n * kWaves) * kTile + 16 * u) & (ps - 1);
+      const int at = (start + (wave + n * WAVES) * kTile + 16 * u) & (ps - 1);
       const char *head = head_of(x.page[u]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) x.code[blk][4 * u + i] = V::load(head + Lay::values(ps) + at * Lay::kRow, 4 * g + i, r, blk);
@@ -175,7 +237,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_mxfp4_kernel(const int32
     if (r >= live || K::dim(st, g) >= HD) qf[st] = u32x4{0, 0, 0, 0};
   }
   for (int n = 0; n < mine; ++n) {
-    const int pos0 = start + (wave + n * kWaves) * kTile;
+    const int pos0 = start + (wave + n * WAVES) * kTile;
     // tokens that do not count: no page, past the end, before the window
     const bool paged[2] = {x.page[0] >= 0, x.page[1] >= 0};
     const bool whole = paged[0] && paged[1] && pos0 >= sr.first && pos0 + kTile <= end;
@@ -246,18 +308,67 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_mxfp4_kernel(const int32
       }
     }
   }
+  if constexpr (WAVES > kWaves) {
+    // the upper half's results go to the lower half, block by block of dimensions
+    float all = sum;
+    all += __shfl_xor(all, 16, 64);
+    all += __shfl_xor(all, 32, 64);
+    const int to = wave & (kWaves - 1);
+    const bool upper = wave >= kWaves;
+    if (upper && g == 0) lds_ml[to][r] = make_float2(m, all);
+    float f = 0.f, f2 = 0.f;
+#pragma unroll
+    for (int blk = 0; blk < V::BLOCKS; ++blk) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int d = (4 * g + i) * V::DPL;
+        if (upper && d < HD / V::BLOCKS)
+#pragma unroll
+          for (int j = 0; j < V::DPL; ++j) lds_o[to][d + j][r] = acc[blk * V::DPL + j][i];
+      }
+      __syncthreads();
+      if (!upper) {
+        if (blk == 0) {
+          const float2 other = lds_ml[to][r];
+          const float top = fmaxf(m, other.x);
+          f = part_factor(make_float2(m, all), top), f2 = part_factor(other, top);
+          sum = sum * f + (g == 0 ? other.y * f2 : 0.f);
+          m = top;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int d = (4 * g + i) * V::DPL;
+          if (d < HD / V::BLOCKS)
+#pragma unroll
+            for (int j = 0; j < V::DPL; ++j) {
+              f32x4 &x = acc[blk * V::DPL + j];
+              x[i] = fmaf(f2, lds_o[to][d + j][r], f * x[i]);
+            }
+        }
+      }
+      __syncthreads();
+    }
+  }
   const int h = threadIdx.x & 15;
   const int64_t head = (int64_t)b * n_heads + (int64_t)kv * group + rt * 16 + h;
   const int64_t slot = (int64_t)item * n_heads + kv * group + rt * 16 + h;       // of a part that is one of several
-  finish_part<HD, V::DPL, V::BLOCKS>(o, part, acc, m, sum, 1.f, wave, live, head, slot, lds_o, lds_ml);
+  finish_part<HD, V::DPL, V::BLOCKS, WAVES>(o, part, acc, m, sum, 1.f, wave, live, head, slot, lds_o, lds_ml);
 }
 
 int launch_paged_mxfp4(int head_dim, const PagedLaunch &l) {
+  const int span = l.window > 0 ? std::min(l.bound, l.window + 15) : l.bound;
+  // Eight wavefronts where a part is long and a compute unit has one at most, us with eight / four: 9 x 2048 of 24 heads of 128 15.3 / 16.7, of 64
+  // 12.3 / 15.1, 32 x 800 of 8 heads of 128 9.1 / 9.5; but 32 x 200 of 4 6.2 / 5.5, 64 x 1500 of 8 24.4 / 20.0.
+  const bool wide = l.share == 0 && span > 512 && l.blocks <= 256;
   return kv_dispatch_mxfp4(head_dim, [&](auto hd) {
-    (l.n_seqs == 1 ? paged_mxfp4_kernel<hd.value, true> : paged_mxfp4_kernel<hd.value, false>)<<<l.blocks, 64 * kWaves, 0, l.stream>>>(
-        l.len, l.table, l.n_seqs, l.share, l.bound, l.window, l.units, l.row_tiles, l.page_shift, l.table_stride, l.group, l.more);
-    ET_LAUNCH_CHECK();
-    return ET_OK;
+    auto launch = [&](auto kernel, int waves) {
+      kernel<<<l.blocks, 64 * waves, 0, l.stream>>>(l.len, l.table, l.n_seqs, l.share, l.bound, l.window, l.units, l.row_tiles, l.page_shift,
+                                                    l.table_stride, l.group, l.more);
+      ET_LAUNCH_CHECK();
+      return ET_OK;
+    };
+    if (wide) return launch(paged_mxfp4_kernel<hd.value, false, 2 * kWaves>, 2 * kWaves);
+    return l.n_seqs == 1 ? launch(paged_mxfp4_kernel<hd.value, true, kWaves>, kWaves) : launch(paged_mxfp4_kernel<hd.value, false, kWaves>, kWaves);
   });
 }
 

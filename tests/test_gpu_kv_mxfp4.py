@@ -166,6 +166,20 @@ def test_attention_leaves_out_what_has_no_page():
     assert not got[1:4].any() and got[0].any() and got[4].any()
 
 
+def test_long_parts_leave_out_what_has_no_page():
+    """The same where eight wavefronts share a part: holes all over, a sequence without any page, places of NaN around."""
+    rng = np.random.default_rng(21)
+    lens, page, kv = [650, 600, 20, 0, 530, 64, 1, 300], 16, 8
+    holes = [(0, i) for i in range(0, 41, 3)] + [(1, i) for i in range(38)] + [(4, i) for i in range(2, 34)] + [(7, 18), (2, 0)]
+    table, n_pages = tables(rng, lens, page, holes=holes)
+    host = Pages4(n_pages, page, kv, 64)
+    tokens = fill(host, table, lens, rng)
+    q = bf16(rng.normal(size=(len(lens), kv, 64)))
+    got = check_attention(host, table, lens, tokens, q, kv, max_len=1024)
+    assert not got[1].any() and not got[3].any() and got[0].any() and got[2].any()
+    check_attention(host, table, lens, tokens, q, kv, window=530, max_len=1024)
+
+
 @pytest.mark.parametrize("size", [0.01, 8.0, 60.0])
 def test_attention_with_small_and_large_logits(size):
     """Nearly equal weights, and logits of thousands whose maximum moves all the time."""
@@ -274,6 +288,9 @@ def held(x):
     return torch.cat(out, -1)
 
 
+MIDDLE = [1000, 0, 1, 33, 513, 700, 128, 129, 255, 1023, 64, 900]
+
+
 @pytest.mark.parametrize("page,kv,heads,d,lens,window", [
     (16, 2, 8, 64, [0, 1, 700, 33, 129, 16, 0, 511] * 19, 0),         # 152 sequences: their lengths are scanned in three steps
     (32, 1, 5, 80, list(range(0, 130)), 0),
@@ -286,6 +303,10 @@ def held(x):
     (16, 64, 64, 64, [45000], 0),                                     # parts of more than 64 groups of 16 tokens a wavefront
     (64, 64, 64, 80, [61000, 61003, 4], 0),
     (64, 4, 4, 128, [70] * 4100, 0),                                  # more than 4096 sequences are one part each
+    # one part each by eight wavefronts, of every head width, several row tiles, a window
+    (16, 8, 16, 64, MIDDLE, 0), (32, 8, 8, 80, MIDDLE, 0), (64, 8, 24, 96, MIDDLE, 0), (16, 8, 8, 128, MIDDLE, 600), (128, 8, 16, 256, MIDDLE, 0),
+    (16, 8, 144, 128, MIDDLE, 0), (16, 24, 24, 80, [9001, 5000, 2047, 2048, 2049, 1, 0, 3000, 2100], 2047),
+    (64, 8, 8, 64, [2048, 5, 1999, 0] * 16, 0),                       # and by four
 ])
 def test_attention_of_many_and_of_long_sequences(page, kv, heads, d, lens, window):
     """Against float64 on what the cache holds, with the bound of check_attention."""
