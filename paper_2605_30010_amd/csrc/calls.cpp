@@ -174,7 +174,7 @@ CALL(attend) {
   const int64_t most = whole(arg[5], INT32_MAX), window = whole(arg[6], INT32_MAX);
   if (!q.t || !seqs.good || q.n != seqs.s.n_seqs || q.heads > INT32_MAX || most < 0 || window < 0 || !PyFloat_CheckExact(arg[7])) Py_RETURN_NONE;
   const float scale = (float)PyFloat_AS_DOUBLE(arg[7]);
-  const at::Tensor out = fresh(q.t->sizes(), at::kBFloat16, device);
+  const at::Tensor out = fresh({q.n, q.heads * cache->head_dim}, at::kBFloat16, device);
   const size_t need = lib.attention_bytes(cache, &seqs.s, (int32_t)q.heads, (int32_t)most, (int32_t)window);
   at::Tensor ws;
   if (need) ws = fresh({(int64_t)need}, at::kByte, device);
