@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
+#include <utility>
 
 #include "mfma_common.h"
 
@@ -138,6 +139,21 @@ static int check_rows(const et_rotary_rows *r, const char *name, int head_dim, i
   return ET_OK;
 }
 
+// Whether rows of `width` values at p (stride between rows) and at q have values in common.  Columns of one wider matrix have the same stride and
+// keep apart within it; rows of different strides have to be apart as a whole.
+struct Span {
+  const uint16_t *p;
+  int64_t stride, width;
+};
+static bool overlap(Span x, Span y, int rows) {
+  if (x.p > y.p) std::swap(x, y);
+  const int64_t off = ((uintptr_t)y.p - (uintptr_t)x.p + 1) / 2;
+  if (off >= (__int128)(rows - 1) * x.stride + x.width) return false;
+  if (rows == 1 || x.stride != y.stride) return true;
+  const int64_t at = off % x.stride;
+  return at < x.width || at + y.width > x.stride;
+}
+
 static constexpr int kMaxHead = 512;                      // (a unit of two values a lane: a head is at most one workgroup)
 // A launch takes fewer than 2^32 lanes, 256 a workgroup of up to 8 rows.
 static constexpr int kMaxRows = 8 * ((1 << 24) - 1);
@@ -199,6 +215,15 @@ int et_rotary_apply(const et_rotary *rotary, const int32_t *positions_dev, int32
   if ((rc = check_rows(q, "q", r.head_dim, rows)) || (rc = check_rows(&kr, "k", r.head_dim, rows))) return rc;
   const int heads = q->n_heads + kr.n_heads;
   if (rows == 0 || heads == 0) return ET_OK;
+  // What is written may be read as the same tensor's values only, and is written once.
+  const Span spans[2][2] = {{{q->in_dev, q->in_stride, (int64_t)q->n_heads * r.head_dim}, {q->out_dev, q->out_stride, (int64_t)q->n_heads * r.head_dim}},
+                            {{kr.in_dev, kr.in_stride, (int64_t)kr.n_heads * r.head_dim}, {kr.out_dev, kr.out_stride, (int64_t)kr.n_heads * r.head_dim}}};
+  for (int i = 0; i < 2; ++i) {
+    const Span &in = spans[i][0], &out = spans[i][1], &other = spans[1 - i][1];
+    if (in.width == 0) continue;
+    ET_REQUIRE(in.p == out.p || !overlap(in, out, rows), "%s has its result in part where it lies itself", i ? "k" : "q");
+    ET_REQUIRE(other.width == 0 || (!overlap(in, other, rows) && !overlap(out, other, rows)), "the result of %s lies on %s", i ? "q" : "k", i ? "k" : "q");
+  }
   ET_REQUIRE(positions_dev != nullptr && r.steps_dev != nullptr && (uintptr_t)r.steps_dev % 8 == 0,
              "positions_dev or steps_dev is NULL or steps_dev is not aligned to 8 bytes");
   const int pairs = r.rot_dim / 2;

@@ -181,3 +181,23 @@ def test_replayed_and_on_other_streams():
     got = [r.apply(q, k, pos, stream=s) for s in streams for _ in range(5)]
     torch.cuda.synchronize()
     assert all(torch.equal(x, c) and torch.equal(y, d) for x, y in got)
+
+
+def test_columns_of_one_matrix():
+    """Queries, keys and values side by side: turned in place, or from some columns into others of the same rows."""
+    rows, heads, kv, d = 9, 4, 2, 64
+    g = torch.Generator("cuda:0").manual_seed(4)
+    r, pos = et.Rotary(d), torch.arange(5, 5 + rows, dtype=torch.int32, device="cuda:0")
+    fused = torch.randn((rows, (2 * heads + 2 * kv) * d), generator=g, device="cuda:0").to(torch.bfloat16)
+    q, k = fused[:, :heads * d], fused[:, heads * d:(heads + kv) * d]
+    want, kept = r.apply(q, k, pos), fused.clone()
+    to = fused[:, (heads + 2 * kv) * d:]
+    got = r.apply(q, None, pos, out=(to, None))[0]
+    assert got is to and torch.equal(to, want[0]) and torch.equal(fused[:, :(heads + 2 * kv) * d], kept[:, :(heads + 2 * kv) * d])
+    r.apply(q, k, pos, out=(q, k))
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and torch.equal(fused[:, (heads + kv) * d:(heads + 2 * kv) * d], kept[:, (heads + kv) * d:(heads + 2 * kv) * d])
+    for a, b, out in ((q, q, (q, q)), (q, None, (fused[:, 1:heads * d + 1], None)), (k, k, (k, None)), (q, k, (to, fused[:, -kv * d:]))):
+        with pytest.raises(et.EtError):
+            r.apply(a, b, pos, out=out)
+    both = r.apply(q, q, pos)                             # one tensor as both is fine where nothing of it is written
+    assert torch.equal(both[0], both[1])

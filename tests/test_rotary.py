@@ -97,3 +97,15 @@ def test_binding_refuses_shapes():
             r.apply(q, None, p)
     with pytest.raises(ValueError):
         r.apply(x, None, pos, out=(x[:, :64], None))
+
+
+def test_refuses_results_that_lie_on_something_else():
+    """Two results in one place, a result on the other's rows or in part on its own; columns of one matrix keep apart (no row: nothing runs)."""
+    at, row = FAKE * 16, dict(in_stride=1024, out_stride=1024)            # 4 heads of 64: 256 of 1024 columns
+    q = dict(row, in_dev=at, out_dev=at)
+    for k in (dict(out_dev=at), dict(in_dev=at), dict(out_dev=at + 2 * 255), dict(in_dev=at + 2 * 1024 * 2 - 2), dict(out_dev=at - 2 * 255), dict(out_stride=1025),
+              dict(out_dev=at + 2 * 1024 - 2)):
+        k = dict(dict(row, in_dev=at + 2 * 256, out_dev=at + 2 * 512), **k)
+        assert call(q=q, k=k) == -1 and "lies on" in et.et_last_error(), k
+    for out, stride in ((at + 2, 1024), (at + 2 * 255, 1024), (at - 2 * 769, 1024), (at + 2 * 256, 1000)):
+        assert call(q=dict(in_dev=at, in_stride=1024, out_dev=out, out_stride=stride)) == -1 and "itself" in et.et_last_error(), (out, stride)
