@@ -256,7 +256,7 @@ __global__ __launch_bounds__(kPoolThreads) void pool_plan_kernel(const int32_t *
 // Then many fill tables, positions and places.  A wavefront takes 64 consecutive rows (or entries) at a time: their sequences lie between
 // the first one's and the last one's, which all lanes look for together.
 __device__ __forceinline__ int find_seq_wave(const int *first, int n_seqs, int x, int total) {
-  const int x0 = __builtin_amdgcn_readfirstlane(x), x1 = min(x0 + 63, total - 1);
+  const int x0 = __builtin_amdgcn_readfirstlane(x), x1 = total - x0 > 64 ? x0 + 63 : total - 1;
   const int lo = find_seq_all(first, 0, n_seqs, x0);
   return find_seq(first, lo, find_seq_all(first, lo, n_seqs, x1), min(x, x1));
 }
