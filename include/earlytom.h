@@ -394,7 +394,8 @@ int et_kv_append(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t
                  const uint16_t *k_dev, int64_t k_stride, const uint16_t *v_dev, int64_t v_stride, void *hip_stream);
 
 /* The same for rows whose places the caller has: row i goes to token slots_dev[i] % page_size of page slots_dev[i] / page_size;
- * a negative slot, or one past the last page, is no place and its row is not stored.  (int64: et_kv_resize makes them.) */
+ * a negative slot, or one past the last page, is no place and its row is not stored.  (int64: et_kv_resize makes them.)  Slots that
+ * are places differ from one another: where they do not, that token holds a mixture of their rows. */
 int et_kv_append_slots(const et_kv_cache *cache, const int64_t *slots_dev, int32_t rows, const uint16_t *k_dev, int64_t k_stride,
                        const uint16_t *v_dev, int64_t v_stride, void *hip_stream);
 
@@ -485,7 +486,7 @@ typedef struct {
 typedef struct {
   const uint16_t *in_dev; /* bf16 [rows, n_heads * head_dim], row stride in_stride (elements)        */
   int64_t in_stride;
-  uint16_t *out_dev; /* may be in_dev, with the same stride; must not overlap it otherwise           */
+  uint16_t *out_dev; /* may be in_dev, with the same stride; otherwise apart from all of q and k     */
   int64_t out_stride;
   int32_t n_heads;
 } et_rotary_rows;

@@ -832,6 +832,8 @@ class PagePool(_OnDevice):
         if len(shape) != 2 or shape[1] < 1 or (strides[1] != 1 and shape[1] > 1):
             raise ValueError("page_table must be [n_seqs, pages] with contiguous rows")
         n, pages = shape
+        if n > 1 and strides[0] > _INT_MAX:
+            raise ValueError("rows of page_table are %d apart: 2^31 - 1 is the most" % strides[0])
         for t, name in ((kv_len, "kv_len"), (new_len, "new_len")):
             if self._ints(t, name).shape != (n,) or not t.is_contiguous():
                 raise ValueError("%s must be contiguous, one for each row of page_table" % name)
@@ -928,6 +930,8 @@ class Rotary(_OnDevice):
         if len(rows) != 1 or not positions.is_contiguous():
             raise ValueError("positions must be contiguous, one for each row")
         rows, d = rows[0], self.head_dim
+        if rows > _INT_MAX:
+            raise ValueError("%d rows: 2^27 - 8 are the most" % rows)
         at, heads, stride = self._heads(q, "q", rows, d)
         if out is None or out[0] is None:
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
@@ -968,6 +972,8 @@ class Rotary(_OnDevice):
             raise ValueError("%s must be [rows, heads * %d] or [rows, heads, %d] with contiguous rows" % (name, d, d))
         if shape[0] != rows:
             raise ValueError("%s has %d rows for %d positions" % (name, shape[0], rows))
+        if heads > 65536:
+            raise ValueError("%s has %d heads: 65536 are the most" % (name, heads))
         return t.data_ptr(), heads, strides[0] if rows > 1 else heads * d
 
 
