@@ -433,3 +433,31 @@ def test_calls_on_several_streams_at_once():
     assert all(torch.equal(t, ref[i]) for i in range(2) for t in got[i])
     back = cache.read(*args, cu, 6300)
     assert torch.equal(back[0], read[0]) and torch.equal(back[1], read[1]) and torch.equal(back[0], -back[1])
+
+
+@pytest.mark.parametrize("kv,heads,d,lens,bound", [(8, 8, 80, [700, 650, 900, 1], 1024),      # one part each by eight wavefronts
+                                                   (2, 6, 96, [9000, 40, 5000], 9000),         # several parts, joined
+                                                   (1, 2, 256, [3000], 3000)])
+def test_blocks_that_are_not_numbers_in_long_sequences(kv, heads, d, lens, bound):
+    """As above where wavefronts, or parts, are added up: a block of NaN stays in its 32 dimensions of a value and in its head of a key."""
+    rng = np.random.default_rng(27)
+    page, nb = 16, O.mx_blocks(d)
+    table, n_pages = tables(rng, lens, page)
+    cache = et.KVCache(n_pages, page, kv, d, fmt="mxfp4")
+    x = torch.randn((sum(lens), 2 * kv * d), generator=torch.Generator("cuda:0").manual_seed(27), device="cuda:0").to(torch.bfloat16)
+    args = dev(table), dev(np.array(lens, dtype=np.int32))
+    cache.append(x[:, :kv * d], x[:, kv * d:], *args, dev(np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)))
+    q = torch.randn((len(lens), heads * d), generator=torch.Generator("cuda:0").manual_seed(28), device="cuda:0").to(torch.bfloat16)
+    clean = dev_to_f64(cache.attend(q, *args, bound)).reshape(len(lens), kv, heads // kv, d)
+    host, kept = Pages4(n_pages, page, kv, d), cache.data.clone()
+    assert np.isfinite(clean).all()
+    for block, pos in ((0, 0), (nb - 1, lens[0] - 1), (nb // 2, lens[0] // 2)):
+        for value in (False, True):
+            p, at = O.place(pos, table[0], n_pages, page)
+            exps = np.arange(host.data.shape[1])[host.cells(at, kv - 1, value)[1]]
+            cache.data.copy_(kept)
+            cache.data[int(p), int(exps[block])] = 255
+            got = dev_to_f64(cache.attend(q, *args, bound)).reshape(clean.shape)
+            hit = np.zeros(clean.shape, dtype=bool)
+            hit[0, kv - 1] = np.arange(d) // 32 == block if value else True
+            assert np.isnan(got[hit]).all() and np.array_equal(got[~hit], clean[~hit])
