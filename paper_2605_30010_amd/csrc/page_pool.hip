@@ -331,9 +331,12 @@ int et_kv_resize(const et_kv_pool *pool, const int32_t *state_dev, int32_t *stat
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const PoolArgs a{pool->ring_dev, page_table_dev, kv_len_dev, new_len_dev, pool->n_pages, __builtin_ctz(page), table_stride, pages_per_seq, n_seqs};
   if (!need) {
-    // one workgroup for a decoding step; more for rows by the thousand
-    const int fillers = (int)std::min<int64_t>(255, ((int64_t)std::max(rows, n_seqs) + 2 * kPoolThreads - 1) / (2 * kPoolThreads));
-    const bool one = fillers <= 1, apart = !one && state_out_dev == state_dev;
+    // A turn of 1024 rows a workgroup, and one that gives; where the new state takes the old one's place, and the giving a launch of its own (3 us),
+    // one workgroup for everything up to six turns.  us, one / several: 4 sequences, 1544 rows 4.9 / 4.6; 256, 2634 7.0 / 5.1, in place 7.0 / 8.2; in
+    // place 4, 5516 7.3 / 7.8; 16, 8550 10.4 / 7.8; 4096, 4096 11.5 / 12.8.  With turns of 2048 rows 16 sequences, 62 605 rows 4.8 -> 5.7,
+    // 1000, 8000 5.7 -> 6.8.
+    const int turns = (int)(((int64_t)std::max(rows, n_seqs) + kPoolThreads - 1) / kPoolThreads), fillers = std::min(255, turns);
+    const bool one = turns <= (state_out_dev == state_dev ? 6 : 1), apart = !one && state_out_dev == state_dev;
     auto launch = [&](int blocks, int what) {
       (n_seqs <= kPoolThreads ? pool_resize_kernel<1> : pool_resize_kernel<4>)<<<blocks, kPoolThreads, 0, stream>>>(
           state_dev, kv_len_dev, new_len_dev, rows, what, a, state_out_dev, cu_rows_dev, positions_dev, slots_dev);

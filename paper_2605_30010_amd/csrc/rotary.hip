@@ -237,7 +237,11 @@ int et_rotary_apply(const et_rotary *rotary, const int32_t *positions_dev, int32
   const bool in_place = (q->n_heads == 0 || q->in_dev == q->out_dev) && (kr.n_heads == 0 || kr.in_dev == kr.out_dev);
   RotaryArgs a{{q->in_dev, q->in_stride, q->out_dev, q->out_stride}, {kr.in_dev, kr.in_stride, kr.out_dev, kr.out_stride}, r.steps_dev, q->n_heads,
                heads, r.head_dim, pairs, (in_place ? r.rot_dim : r.head_dim) / (2 * vec), r.amplitude, transpose ? -1.f : 1.f};
-  const int per_block = std::max(1, std::min(8, rows / 512));
+  // Rows of a workgroup: as many as give its lanes fewer than two units each, at most 8, and 512 workgroups at least.  Wide rows gain nothing by
+  // sharing one: us at one / 2 / 4 / 8 rows of 32 heads of 128 (256 units), 65 536 rows 191 / 193 / 197 / 205, 300 rows 3.1 / 3.3 / 4.0 / 5.8; of 40
+  // interleaved heads of 80 (400 units) 168 / 174 / 194 / 218; but of 5 heads of 64 (20 units) 46.8 / 26.0 / 19.4 / 14.9.  With fewer than
+  // one unit a lane instead: 65 536 rows of 4 heads of 80 in units of 4 (80 units) 21.3 -> 27.1, of 16 heads of 64 39.4 -> 41.0.
+  const int per_block = std::max(1, std::min({8, rows / 512, 511 / (heads * a.units)}));
   const unsigned blocks = (unsigned)((rows + per_block - 1) / per_block);
   const size_t lds = (size_t)per_block * pairs * 2 * sizeof(float);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
