@@ -100,9 +100,10 @@ static PagedPlan paged_plan(const et_kv_cache &c, const et_kv_seqs &s, int n_hea
   // 1419 / 1261 (of one key-value head 1113 / 277).
   const int64_t all = (int64_t)s.n_seqs * p.units;
   // In 4 bits a part's tokens are a quarter of the bytes, and the same rule holds up to 2048 tokens (and a window's 15 more) from 192 on: one part
-  // each / shared out, heads of 128, 9 x 2048 of 24 15.3 / 19.7, 64 x 1500 of 8 20.0 / 28.1, 64 x 2048 25.0 / 32.1, 64 x 64 to 2048 23.5 / 22.5;
-  // but 32 x 2048 of 4 14.6 / 13.9, 64 x 64 to 4096 of 8 40.0 / 34.1.
-  const bool whole = span <= 512 || (span <= 1024 && all >= 64) || (c.format == ET_KV_MXFP4 ? span <= 2063 && all >= 192 : span <= 2048 && all >= 1024) || s.n_seqs > 4096;
+  // each / shared out, heads of 128, 9 x 2048 of 24 13.9 / 18.1, 64 x 1500 of 8 19.2 / 25.3, 64 x 2048 24.0 / 28.3, 64 x 64 to 2048 21.1 / 20.6;
+  // but 32 x 2048 of 4 12.7 / 12.3, 64 x 64 to 4096 of 8 36.1 / 32.9.
+  const bool full = c.format == ET_KV_MXFP4 ? span <= 2063 && all >= 192 : span <= 2048 && all >= 1024;
+  const bool whole = span <= 512 || (span <= 1024 && all >= 64) || full || s.n_seqs > 4096;
   p.share = whole ? 0 : (int)std::min<int64_t>(blocks, (kShare + p.units - 1) / p.units);
   p.items = p.share * (s.n_seqs > 1 ? kFiner : 1) + (int64_t)s.n_seqs;
   p.slots = p.share ? (size_t)p.items * n_heads : 0;

@@ -79,29 +79,44 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
+// What lane r's column of the products is: COLS columns are one query head's, r / COLS.  One: column h is head h, and an accumulator's rows
+// are the j-th of DPL dimensions each.  Two: the even and the odd dimensions; a row of the values' operand is then a pair of dimensions as
+// codes become them, (token, even), (token, odd) in turn along the summed axis, and a weight stands in the place of its column's parity, 0 in
+// the other.  Four: both, with a weight's two halves apart.
+template <int COLS>
+struct Cols {
+  static constexpr int WIDTH = COLS == 1 ? 1 : 2;         // dimensions of an operand's row
+  int head, odd, low;
+  bool first, writes;                                     // of the head's columns; of those that are added up
+  __device__ __forceinline__ Cols(int r)
+      : head(r / COLS), odd(COLS == 1 ? 0 : r & 1), low(COLS == 4 ? r >> 1 & 1 : 0), first(r % COLS == 0), writes(!low) {}
+  __device__ __forceinline__ int dim(int j) const { return j * WIDTH + odd; }
+};
+
 // The end of a workgroup's part: its wavefronts' results (accumulators, reference m and this lane's sum of query head r) together, and out,
 // or to where the parts are joined.  `factor`: what the values are multiplied with.  WAVES: wavefronts of the workgroup, of which the first kWaves
 // have results.
-template <int HD, int DPL, int BLOCKS, int WAVES>
-__device__ __forceinline__ void finish_part(const PagedMore &o, const Part &part, const f32x4 (&acc)[BLOCKS * DPL], float m, float sum, float factor,
+template <int HD, int DPL, int BLOCKS, int WAVES, int COLS>
+__device__ __forceinline__ void finish_part(const PagedMore &o, const Part &part, const f32x4 (&acc)[BLOCKS * DPL / Cols<COLS>::WIDTH], float m, float sum, float factor,
                                             int wave, int live, int64_t head, int64_t slot, float (&lds_o)[kWaves][HD / BLOCKS][16],
                                             float2 (&lds_ml)[kWaves][16]) {
   constexpr int BD = HD / BLOCKS;                         // dimensions that the wavefronts add up at a time
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, h = threadIdx.x & 15;
   sum += __shfl_xor(sum, 16, 64);
   sum += __shfl_xor(sum, 32, 64);
-  if (g == 0 && (WAVES == kWaves || wave < kWaves)) lds_ml[wave][r] = make_float2(m, sum);
+  const Cols<COLS> col(r);
+  if (g == 0 && col.first && (WAVES == kWaves || wave < kWaves)) lds_ml[wave][col.head] = make_float2(m, sum);
   float top = -INFINITY, total = 0.f, f[kWaves];
 #pragma unroll
   for (int blk = 0; blk < BLOCKS; ++blk) {
     if (blk) __syncthreads();
-    if (r < live && (WAVES == kWaves || wave < kWaves)) {
+    if (col.writes && col.head < live && (WAVES == kWaves || wave < kWaves)) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int d = (4 * g + e) * DPL;
         if (d < BD)
 #pragma unroll
-          for (int j = 0; j < DPL; ++j) lds_o[wave][d + j][r] = acc[blk * DPL + j][e];
+          for (int j = 0; j < DPL / col.WIDTH; ++j) lds_o[wave][d + col.dim(j)][col.head] = acc[blk * DPL / col.WIDTH + j][e];
       }
     }
     __syncthreads();
@@ -141,19 +156,20 @@ __device__ __forceinline__ void finish_part(const PagedMore &o, const Part &part
 
 // As paged_attention_kernel: a workgroup takes one part of a sequence's tokens for up to 16 query heads of one key-value head, its
 // wavefronts tiles of 32 tokens in turn, S^T = K Q^T and O^T += V^T P^T by matrix instructions on bfloat16 numbers, which codes and their power of two
-// are exactly; a weight is the sum of two of them.  A tile's registers are loaded again as soon as they have become operands, so the next
+// are exactly; a weight is the sum of two of them, within 2^-14 (2^-15 where a head has one column).  A tile's registers are loaded again as soon as they have become operands, so the next
 // tile's keys come in during the softmax and the second product, its values during that and the next logits.
-template <int HD, bool ONE, int WAVES>
+template <int HD, bool ONE, int WAVES, int COLS>
 __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_t *len, const int32_t *table, int n_seqs, int share, int bound,
                                                                  int window, int units, int row_tiles, int page_shift, int table_stride,
                                                                  int group, PagedMore o) {
   using Lay = KvLayout<HD, ET_KV_MXFP4>;
   using K = MxKeys<HD>;
   using V = MxValues<HD>;
-  constexpr int ACC = V::BLOCKS * V::DPL;
+  constexpr int ACCS = V::DPL / Cols<COLS>::WIDTH, ACC = V::BLOCKS * ACCS;
   __shared__ float lds_o[kWaves][HD / V::BLOCKS][16];
   __shared__ float2 lds_ml[kWaves][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const Cols<COLS> col(r);
   const PagedArgs a{len, n_seqs, bound, window, share};
   // (row tiles of one part and key-value head eight workgroups apart, as there)
   const int kv_heads = units / row_tiles;
@@ -224,7 +240,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
   u32x4 qf[K::STEPS];
 #pragma unroll
   for (int st = 0; st < K::STEPS; ++st)
-    qf[st] = *reinterpret_cast<const u32x4 *>(o.q + b * o.q_stride + ((int64_t)kv * group + rt * 16 + min(r, live - 1)) * HD +
+    qf[st] = *reinterpret_cast<const u32x4 *>(o.q + b * o.q_stride + ((int64_t)kv * group + rt * 16 + min(col.head, live - 1)) * HD +
                                               min(K::dim(st, g), HD - 8));
   if (mine > 0) {
     load_keys(0);
@@ -234,8 +250,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
 #pragma unroll
   for (int st = 0; st < K::STEPS; ++st) {
     asm volatile("" : "+v"(qf[st]));
-    if (r >= live || K::dim(st, g) >= HD) qf[st] = u32x4{0, 0, 0, 0};
+    if (col.head >= live || K::dim(st, g) >= HD) qf[st] = u32x4{0, 0, 0, 0};
   }
+  const uint32_t half = col.odd ? 0x03020C0Cu : 0x0C0C0302u;              // (a number's upper half in the place of its parity)
+  const uint32_t cut = col.low ? 0xFFFF0000u : 0;
   for (int n = 0; n < mine; ++n) {
     const int pos0 = start + (wave + n * WAVES) * kTile;
     // tokens that do not count: no page, past the end, before the window
@@ -282,11 +300,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
       sum += p[i];
     }
     // the weights' halves: what bfloat16 cuts off goes into the second
-    u32x4 pf, pl;
+    u32x4 pf[2], pl[2];
+    if constexpr (COLS == 1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      pf[i] = __builtin_amdgcn_perm(__float_as_uint(p[2 * i + 1]), __float_as_uint(p[2 * i]), 0x07060302u);
-      pl[i] = cvt_pk_bf16(p[2 * i] - bf16lo_to_f32(pf[i]), p[2 * i + 1] - bf16hi_to_f32(pf[i]));
+      for (int i = 0; i < 4; ++i) {
+        pf[0][i] = __builtin_amdgcn_perm(__float_as_uint(p[2 * i + 1]), __float_as_uint(p[2 * i]), 0x07060302u);
+        pl[0][i] = cvt_pk_bf16(p[2 * i] - bf16lo_to_f32(pf[0][i]), p[2 * i + 1] - bf16hi_to_f32(pf[0][i]));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float rest = p[i] - __uint_as_float(__float_as_uint(p[i]) & (COLS == 4 ? cut : 0xFFFF0000u));
+        const uint32_t x = COLS == 4 ? __float_as_uint(rest) : __float_as_uint(p[i]);
+        pf[i / 4][i & 3] = __builtin_amdgcn_perm(x, x, half);
+        if constexpr (COLS == 2) pl[i / 4][i & 3] = __builtin_amdgcn_perm(__float_as_uint(rest), __float_as_uint(rest), half);
+      }
     }
 #pragma unroll
     for (int blk = 0; blk < V::BLOCKS; ++blk) {
@@ -301,12 +329,27 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
           for (int j = 0; j < V::NREG; ++j) vw[i][j] = dead >> i & 1 ? 0 : vw[i][j];   // (0 times what lies there could be NaN)
       }
 #pragma unroll
-      for (int j = 0; j < V::DPL; ++j) {
-        const u32x4 values = V::operand(vw, j);
-        f32x4 &to = acc[blk * V::DPL + j];
-        to = mfma16(values, pf, mfma16(values, pl, to));
+      for (int j = 0; j < ACCS; ++j) {
+        f32x4 &to = acc[blk * ACCS + j];
+        if constexpr (COLS == 1) {
+          const u32x4 values = V::operand(vw, j);
+          to = mfma16(values, pf[0], mfma16(values, pl[0], to));
+        } else {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const u32x4 values{vw[4 * u][j], vw[4 * u + 1][j], vw[4 * u + 2][j], vw[4 * u + 3][j]};
+            if constexpr (COLS == 2) to = mfma16(values, pl[u], to);
+            to = mfma16(values, pf[u], to);
+          }
+        }
       }
     }
+  }
+  if constexpr (COLS == 4) {
+#pragma unroll
+    for (int j = 0; j < ACC; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[j][i] += __shfl_xor(acc[j][i], 2, 64);
   }
   if constexpr (WAVES > kWaves) {
     // the upper half's results go to the lower half, block by block of dimensions
@@ -322,9 +365,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int d = (4 * g + i) * V::DPL;
-        if (upper && d < HD / V::BLOCKS)
+        if (upper && col.writes && d < HD / V::BLOCKS)
 #pragma unroll
-          for (int j = 0; j < V::DPL; ++j) lds_o[to][d + j][r] = acc[blk * V::DPL + j][i];
+          for (int j = 0; j < ACCS; ++j) lds_o[to][d + col.dim(j)][col.head] = acc[blk * ACCS + j][i];
       }
       __syncthreads();
       if (!upper) {
@@ -340,9 +383,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
           const int d = (4 * g + i) * V::DPL;
           if (d < HD / V::BLOCKS)
 #pragma unroll
-            for (int j = 0; j < V::DPL; ++j) {
-              f32x4 &x = acc[blk * V::DPL + j];
-              x[i] = fmaf(f2, lds_o[to][d + j][r], f * x[i]);
+            for (int j = 0; j < ACCS; ++j) {
+              f32x4 &x = acc[blk * ACCS + j];
+              x[i] = fmaf(f2, lds_o[to][d + col.dim(j)][col.head], f * x[i]);
             }
         }
       }
@@ -352,13 +395,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
   const int h = threadIdx.x & 15;
   const int64_t head = (int64_t)b * n_heads + (int64_t)kv * group + rt * 16 + h;
   const int64_t slot = (int64_t)item * n_heads + kv * group + rt * 16 + h;       // of a part that is one of several
-  finish_part<HD, V::DPL, V::BLOCKS, WAVES>(o, part, acc, m, sum, 1.f, wave, live, head, slot, lds_o, lds_ml);
+  finish_part<HD, V::DPL, V::BLOCKS, WAVES, COLS>(o, part, acc, m, sum, 1.f, wave, live, head, slot, lds_o, lds_ml);
 }
 
 int launch_paged_mxfp4(int head_dim, const PagedLaunch &l) {
   const int span = l.window > 0 ? std::min(l.bound, l.window + 15) : l.bound;
-  // Eight wavefronts where a part is long and a compute unit has one at most, us with eight / four: 9 x 2048 of 24 heads of 128 15.3 / 16.7, of 64
-  // 12.3 / 15.1, 32 x 800 of 8 heads of 128 9.1 / 9.5; but 32 x 200 of 4 6.2 / 5.5, 64 x 1500 of 8 24.4 / 20.0.
+  // Eight wavefronts where a part is long and a compute unit has one at most, us with eight / four: 9 x 2048 of 24 heads of 128 13.9 / 16.7, of 64
+  // 11.3 / 14.2, 32 x 800 of 8 heads of 128 7.8 / 8.9; but 32 x 200 of 4 5.6 / 5.2, 64 x 1500 of 8 20.6 / 19.4.
   const bool wide = l.share == 0 && span > 512 && l.blocks <= 256;
   return kv_dispatch_mxfp4(head_dim, [&](auto hd) {
     auto launch = [&](auto kernel, int waves) {
@@ -367,8 +410,17 @@ int launch_paged_mxfp4(int head_dim, const PagedLaunch &l) {
       ET_LAUNCH_CHECK();
       return ET_OK;
     };
-    if (wide) return launch(paged_mxfp4_kernel<hd.value, false, 2 * kWaves>, 2 * kWaves);
-    return l.n_seqs == 1 ? launch(paged_mxfp4_kernel<hd.value, true, kWaves>, kWaves) : launch(paged_mxfp4_kernel<hd.value, false, kWaves>, kWaves);
+    // As many columns of a head as there is room for.  us with 1 / 2 / 4: 9 x 1 to 2047 tokens of 24 heads of 80 15.5 / 14.6 / 14.0, 32 x 800 of
+    // 8 of 128 with four query heads each 9.0 / 8.3 / 8.2, 32 x 1000 of 4 with seven 9.6 / 8.9; where memory is the bound they are level, 64 x
+    // 1000 to 16384 tokens of 8 122.
+    auto pick = [&](auto cols) {
+      if (wide) return launch(paged_mxfp4_kernel<hd.value, false, 2 * kWaves, cols.value>, 2 * kWaves);
+      return l.n_seqs == 1 ? launch(paged_mxfp4_kernel<hd.value, true, kWaves, cols.value>, kWaves)
+                           : launch(paged_mxfp4_kernel<hd.value, false, kWaves, cols.value>, kWaves);
+    };
+    if (l.group <= 4) return pick(std::integral_constant<int, 4>());
+    if (l.group <= 8) return pick(std::integral_constant<int, 2>());
+    return pick(std::integral_constant<int, 1>());
   });
 }
 

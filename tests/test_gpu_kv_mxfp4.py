@@ -343,6 +343,14 @@ def test_attention_of_many_and_of_long_sequences(page, kv, heads, d, lens, windo
         at += n
 
 
+@pytest.mark.parametrize("d", [64, 80, 96, 128, 256])
+@pytest.mark.parametrize("group", [1, 2, 3, 4, 5, 7, 8, 9, 16, 17])
+def test_every_number_of_query_heads_a_key_value_head(group, d):
+    """Short sequences, several at once and one alone; parts by eight wavefronts; parts that are joined; a window."""
+    for page, kv, lens, window in ((16, 2, [40, 1, 0, 129], 0), (32, 1, [300], 0), (64, 16, [700, 530, 3, 0], 0), (16, 1, [2100, 33], 0), (128, 2, [2500], 1300)):
+        test_attention_of_many_and_of_long_sequences(page, kv, kv * group, d, lens, window)
+
+
 def test_pages_past_four_gigabytes():
     """Pages whose byte offset needs more than 32 bits: stored, read back and attended to."""
     rng = np.random.default_rng(16)
