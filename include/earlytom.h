@@ -414,7 +414,7 @@ int et_kv_read(const et_kv_cache *cache, const et_kv_seqs *seqs, const int32_t *
  * short sequences take a second launch by it (1 x 197 tokens 7.7 instead of 4.8 us, 256 x 500 58 instead of 50, 1024 x 60 97 instead
  * of 33).  Two equal calls give equal bits; a sequence beside others, or under another bound, may be split elsewhere, which moves
  * its result within the rounding.
- * Logits, their maximum, the sums and the products' accumulators are float32, the weights within 2^-15 of that (2^-14 in 4 bits).  Values are summed
+ * Logits, their maximum, the sums and the products' accumulators are float32, the weights within 2^-15 of that.  Values are summed
  * before the division by the weights' sum, and in 8 bits a query's products with the codes before the row's factor, so values and
  * queries beyond 2^100 can overflow; in 8 bits the weights carry the value rows' maxima, so those below 2^-90 lose bits.  Keys
  * and values in 4 bits enter both products as the exact numbers that they stand for.

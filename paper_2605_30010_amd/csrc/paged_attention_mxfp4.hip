@@ -1,5 +1,6 @@
 // Attention of one new token per sequence over a paged key-value cache in 4 bits.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged_attention.h"
 
@@ -82,15 +83,26 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // What lane r's column of the products is: COLS columns are one query head's, r / COLS.  One: column h is head h, and an accumulator's rows
 // are the j-th of DPL dimensions each.  Two: the even and the odd dimensions; a row of the values' operand is then a pair of dimensions as
 // codes become them, (token, even), (token, odd) in turn along the summed axis, and a weight stands in the place of its column's parity, 0 in
-// the other.  Four: both, with a weight's two halves apart.
+// the other.  Four: both, with a weight's two halves apart.  A head's columns have the same logits; each takes a share of their softmax.
 template <int COLS>
 struct Cols {
   static constexpr int WIDTH = COLS == 1 ? 1 : 2;         // dimensions of an operand's row
-  int head, odd, low;
+  int head, index, odd, low;
   bool first, writes;                                     // of the head's columns; of those that are added up
   __device__ __forceinline__ Cols(int r)
-      : head(r / COLS), odd(COLS == 1 ? 0 : r & 1), low(COLS == 4 ? r >> 1 & 1 : 0), first(r % COLS == 0), writes(!low) {}
+      : head(r / COLS), index(r % COLS), odd(COLS == 1 ? 0 : r & 1), low(COLS == 4 ? r >> 1 & 1 : 0), first(index == 0), writes(!low) {}
   __device__ __forceinline__ int dim(int j) const { return j * WIDTH + odd; }
+  // of four logits that all columns of a head have: the i-th of the column's own
+  __device__ __forceinline__ float pick(f32x4 d, int i) const {
+    if constexpr (COLS == 1) return d[i];
+    else if constexpr (COLS == 2) return odd ? d[2 * i + 1] : d[2 * i];
+    else return low ? (odd ? d[3] : d[2]) : (odd ? d[1] : d[0]);
+  }
+  // what the head's column I has
+  template <int I>
+  __device__ __forceinline__ uint32_t from(uint32_t x) const {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, COLS == 4 ? I * 0x55 : I * 0x55 + 0xA0, 0xf, 0xf, true);
+  }
 };
 
 // The end of a workgroup's part: its wavefronts' results (accumulators, reference m and this lane's sum of query head r) together, and out,
@@ -156,7 +168,7 @@ __device__ __forceinline__ void finish_part(const PagedMore &o, const Part &part
 
 // As paged_attention_kernel: a workgroup takes one part of a sequence's tokens for up to 16 query heads of one key-value head, its
 // wavefronts tiles of 32 tokens in turn, S^T = K Q^T and O^T += V^T P^T by matrix instructions on bfloat16 numbers, which codes and their power of two
-// are exactly; a weight is the sum of two of them, within 2^-14 (2^-15 where a head has one column).  A tile's registers are loaded again as soon as they have become operands, so the next
+// are exactly; a weight is the sum of two of them, within 2^-15.  A tile's registers are loaded again as soon as they have become operands, so the next
 // tile's keys come in during the softmax and the second product, its values during that and the next logits.
 template <int HD, bool ONE, int WAVES, int COLS>
 __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_t *len, const int32_t *table, int n_seqs, int share, int bound,
@@ -165,7 +177,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
   using Lay = KvLayout<HD, ET_KV_MXFP4>;
   using K = MxKeys<HD>;
   using V = MxValues<HD>;
-  constexpr int ACCS = V::DPL / Cols<COLS>::WIDTH, ACC = V::BLOCKS * ACCS;
+  constexpr int ACCS = V::DPL / Cols<COLS>::WIDTH, ACC = V::BLOCKS * ACCS, OWN = 8 / COLS;
   __shared__ float lds_o[kWaves][HD / V::BLOCKS][16];
   __shared__ float2 lds_ml[kWaves][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
@@ -252,22 +264,23 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
     asm volatile("" : "+v"(qf[st]));
     if (col.head >= live || K::dim(st, g) >= HD) qf[st] = u32x4{0, 0, 0, 0};
   }
-  const uint32_t half = col.odd ? 0x03020C0Cu : 0x0C0C0302u;              // (a number's upper half in the place of its parity)
-  const uint32_t cut = col.low ? 0xFFFF0000u : 0;
+  // selectors of a weight's half in the place of the column's parity, 0 in the other: the upper one's (four columns: the column's own), the lower one's
+  const uint32_t half = col.low ? (col.odd ? 0x03020C0Cu : 0x0C0C0302u) : (col.odd ? 0x01000C0Cu : 0x0C0C0100u);
+  const uint32_t half2 = col.odd ? 0x03020C0Cu : 0x0C0C0302u;
   for (int n = 0; n < mine; ++n) {
     const int pos0 = start + (wave + n * WAVES) * kTile;
     // tokens that do not count: no page, past the end, before the window
     const bool paged[2] = {x.page[0] >= 0, x.page[1] >= 0};
     const bool whole = paged[0] && paged[1] && pos0 >= sr.first && pos0 + kTile <= end;
     const int next = min(n + 1, mine - 1);              // (the last tile again, from the caches, so that every turn has the same loads)
-    float z[8];
+    float z[OWN];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       f32x4 d{0, 0, 0, 0};
 #pragma unroll
       for (int st = 0; st < K::STEPS; ++st) d = mfma16(K::operand(x.kw[u], x.ku[u], st, g), qf[st], d);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) z[4 * u + i] = whole_product(d[i], o.scale_log2);
+      for (int i = 0; i < 4 / COLS; ++i) z[4 / COLS * u + i] = whole_product(col.pick(d, i), o.scale_log2);
     }
     load_keys(next);
     uint32_t dead = 0;
@@ -277,13 +290,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
         const int pos = pos0 + 16 * (i / 4) + 4 * g + (i & 3);
         if (!paged[i / 4] || pos < sr.first || pos >= end) {
           dead |= 1u << i;
-          z[i] = -INFINITY;
         }
       }
+#pragma unroll
+      for (int i = 0; i < OWN; ++i)
+        if (dead >> (COLS * i + col.index) & 1) z[i] = -INFINITY;
     }
     // The reference of the exponentials moves when a logit exceeds it by 2^8: below that nothing overflows.
-    float top = max3(max3(z[0], z[1], z[2]), max3(z[3], z[4], z[5]), max3(z[6], z[7], z[7]));
+    float top = max3(z[0], z[1], z[OWN > 2 ? 2 : 1]);
+#pragma unroll
+    for (int i = 3; i < OWN; i += 2) top = max3(top, z[i], z[min(i + 1, OWN - 1)]);
     if (__ballot(top > m + 8.f)) {
+#pragma unroll
+      for (int i = 1; i < COLS; i *= 2) top = fmaxf(top, __shfl_xor(top, i, 64));
       top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
       const float m2 = fmaxf(m, top), f = m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m2);
@@ -293,9 +312,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
       for (int j = 0; j < ACC; ++j) acc[j] *= f;
     }
     const float ref = m == -INFINITY ? 0.f : m;
-    float p[8];
+    float p[OWN];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < OWN; ++i) {
       p[i] = __builtin_amdgcn_exp2f(z[i] - ref);
       sum += p[i];
     }
@@ -308,13 +327,22 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
         pl[0][i] = cvt_pk_bf16(p[2 * i] - bf16lo_to_f32(pf[0][i]), p[2 * i + 1] - bf16hi_to_f32(pf[0][i]));
       }
     } else {
+      // both halves of a lane's weights in one register, which the head's other columns read from there
+      uint32_t both[OWN];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float rest = p[i] - __uint_as_float(__float_as_uint(p[i]) & (COLS == 4 ? cut : 0xFFFF0000u));
-        const uint32_t x = COLS == 4 ? __float_as_uint(rest) : __float_as_uint(p[i]);
-        pf[i / 4][i & 3] = __builtin_amdgcn_perm(x, x, half);
-        if constexpr (COLS == 2) pl[i / 4][i & 3] = __builtin_amdgcn_perm(__float_as_uint(rest), __float_as_uint(rest), half);
+      for (int i = 0; i < OWN; ++i) {
+        const float high = __uint_as_float(__float_as_uint(p[i]) & 0xFFFF0000u);
+        both[i] = cvt_pk_bf16(high, p[i] - high);
       }
+      const auto place = [&](auto token) {
+        constexpr int i = decltype(token)::value;
+        const uint32_t w = col.template from<i % COLS>(both[i / COLS]);
+        pf[i / 4][i & 3] = __builtin_amdgcn_perm(w, w, half);
+        if constexpr (COLS == 2) pl[i / 4][i & 3] = __builtin_amdgcn_perm(w, w, half2);
+      };
+      place(std::integral_constant<int, 0>()), place(std::integral_constant<int, 1>()), place(std::integral_constant<int, 2>());
+      place(std::integral_constant<int, 3>()), place(std::integral_constant<int, 4>()), place(std::integral_constant<int, 5>());
+      place(std::integral_constant<int, 6>()), place(std::integral_constant<int, 7>());
     }
 #pragma unroll
     for (int blk = 0; blk < V::BLOCKS; ++blk) {
@@ -345,6 +373,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
       }
     }
   }
+#pragma unroll
+  for (int i = 1; i < COLS; i *= 2) sum += __shfl_xor(sum, i, 64);
   if constexpr (COLS == 4) {
 #pragma unroll
     for (int j = 0; j < ACC; ++j)
