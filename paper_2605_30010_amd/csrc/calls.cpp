@@ -2,7 +2,7 @@
 // their host part is most of a small call.  A function here makes the call if everything about it is as it mostly is (plain tensors on the
 // device, of the types and layouts asked for) and returns what it makes, or the entry point's error code; for anything else it
 // returns None, and binding.py, which has all the checks and says what is wrong, goes on.  us a call of the binding, launch 2.7 included, without /
-// with this: rotary positions of queries and keys 8.6 / @R, a pool's step 10.0 / @P, rows stored 6.8 / @S, read 8.3 / @L, attention 7.2 / @A.
+// with this: rotary positions of queries and keys 8.6 / 5.6, a pool's step 10.0 / 6.5, rows stored 6.8 / 4.1, read 8.3 / 5.7, attention 7.2 / 5.2.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <dlfcn.h>
