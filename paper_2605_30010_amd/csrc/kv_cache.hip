@@ -191,8 +191,8 @@ __device__ __forceinline__ uint32_t mx_encode8(u32x4 x, uint32_t exponent) {
 // the way to a place is a chain of four loads, so rows share it when there are many.  What is read or written once in long
 // streams (new rows, unquantised cells, rows read back) goes past the caches: 391 MB of e4m3 codes read back 265 -> 254 us, 130 000
 // rows of 4 heads of 80 73 -> 65, 134 MB of bfloat16 rows stored 110 -> 101; codes and the cells of a read do not gain by it.
-// SLOTS: the rows' places are given, in the place of `cu`.  In 4 bits 65 500 rows of 16 heads of 96 are stored in 105 us and read back in 91, 509 MB
-// each way around; the exponents, three bytes of a row that lie `page` bytes apart, cost the store 159 MB written and 403 read for 107 and 403.
+// SLOTS: the rows' places are given, in the place of `cu`.  In 4 bits 65 500 rows of 16 heads of 96 are stored in 105 us and read back in 77: 403 MB of
+// rows and 107 of codes and exponents each way, which is what passes the memory side (403 + 111 MB, 5.7 TB/s for both).
 constexpr int kBatch = 4;
 template <int HD, int FMT, bool STORE, bool SLOTS>
 __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const int32_t *len, const int32_t *table, int n_seqs, int rows,
@@ -201,7 +201,14 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const i
   using Lay = KvLayout<HD, FMT>;
   constexpr int LANES = kv_lanes<HD>(), GROUPS = 256 / LANES;
   __shared__ int4 lds_place[64];                         // byte offset of the page (two words), token of the page, 0 / 1 / 2
-  const int first = blockIdx.x * per_block, count = min(per_block, rows - first);
+  // In 4 bits neighbouring workgroups' rows share cache lines of exponents.  An XCD takes 32 neighbours, so that they meet in its cache: 65 500 rows of
+  // 16 heads of 96 stored and read back 203 -> 182 us, 32 800 of 32 of 80 201 -> 165, others level (8 neighbours 186, 170; an eighth of
+  // all rows 183, 164, but 131 000 of 8 of 128 124 -> 130).
+  int place = blockIdx.x;
+  if constexpr (FMT == ET_KV_MXFP4) {
+    if (place < (int)gridDim.x / 256 * 256) place = place / 256 * 256 + place % 8 * 32 + place / 8 % 32;
+  }
+  const int first = place * per_block, count = min(per_block, rows - first);
   if (threadIdx.x < 64) {
     KvPlace p;
     if constexpr (SLOTS) p = kv_slot(reinterpret_cast<const int64_t *>(cu), first, count, c.n_pages, page_shift);
@@ -342,12 +349,15 @@ static int check_rows(const et_kv_cache *cache, const et_kv_seqs *seqs, const in
 // 128 stored 116 / 110 / 112 / 118 / 118, e4m3 stored and read back 251 / 190 / 177 / 175 / 178; 130 000 bfloat16 rows of 4 heads of 80
 // read 179 / 93 / 73 / 72 / 77; 5000 int8 rows of 4 heads of 128 stored and read back 17.7 / 12.9 / 15.1 / 19.0 / 26.7; at 16 / 32 / 64
 // rows: 928 000 int8 rows of 3 heads of 64 read 293 / 261 / 251, 630 000 of one head of 128 stored and read back 259 / 222 / 220.
-// In 4 bits at 4 / 8 / 16 turns, stored and read back: 65 500 rows of 16 heads of 96 213 / 202 / 202, 65 000 of 4 of 128 66.5 / 66.1 / 68.9,
-// 32 800 of 32 of 80 215 / 201 / 241, 180 000 of 4 of 64 89 / 91 / 100.
+// In 4 bits four turns too, or eight where those are fewer than four rows; stored and read back at 4 / 8 / 16 turns: 16 000 rows of 4 heads of 128
+// 18.8 / 21.2 / 21.2, 131 000 of 8 118 / 122 / 126, 180 000 of 4 of 64 88 / 91 / 101; 65 500 of 16 of 96 193 / 182 / 189, 32 800 of 32 of 80
+// 181 / 165 / 174.
 static int rows_per_block(int rows, const et_kv_cache &c) {
-  const int lanes = c.head_dim <= 64 ? 8 : c.head_dim <= 128 ? 16 : 32, turns = c.format == ET_KV_BF16 ? 4 : c.format == ET_KV_MXFP4 ? 8 : 16;
+  const int lanes = c.head_dim <= 64 ? 8 : c.head_dim <= 128 ? 16 : 32;
+  const auto turns = [&](int n) { return n * (256 / lanes) / (2 * c.n_kv_heads); };
+  const int most = c.format == ET_KV_BF16 ? turns(4) : c.format == ET_KV_MXFP4 ? std::min(turns(8), std::max(turns(4), 4)) : turns(16);
   const int least = (int)(((int64_t)rows + kMaxBlocks - 1) / kMaxBlocks);
-  return std::max(least, std::min({64, rows / 1024, turns * (256 / lanes) / (2 * c.n_kv_heads)}));
+  return std::max(least, std::min({64, rows / 1024, most}));
 }
 
 template <bool STORE>
