@@ -34,28 +34,33 @@ __device__ __forceinline__ void turn(uint32_t t, float &c, float &s) {
   s = quarter & 2 ? -b : b;
 }
 
-// N bfloat16 values as they lie, L of them a load.
+// N bfloat16 values as they lie, L of them a load.  PAST: past the caches.
 template <int L>
 struct Bits;
 template <> struct Bits<1> { using type = uint16_t; };
 template <> struct Bits<2> { using type = uint32_t; };
 template <> struct Bits<4> { using type = uint2; };
-template <> struct Bits<8> { using type = uint4; };
-template <int L, int N>
+template <> struct Bits<8> { using type = u32x4; };
+template <int L, bool PAST, int N>
 __device__ __forceinline__ void load_bits(const uint16_t *p, uint16_t (&v)[N]) {
 #pragma unroll
   for (int i = 0; i < N; i += L) {
-    const auto b = *reinterpret_cast<const typename Bits<L>::type *>(p + i);
+    const auto *from = reinterpret_cast<const typename Bits<L>::type *>(p + i);
+    typename Bits<L>::type b;
+    if constexpr (PAST) b = __builtin_nontemporal_load(from);
+    else b = *from;
     __builtin_memcpy(&v[i], &b, 2 * L);
   }
 }
-template <int L, int N>
+template <int L, bool PAST, int N>
 __device__ __forceinline__ void store_bits(uint16_t *p, const uint16_t (&v)[N]) {
 #pragma unroll
   for (int i = 0; i < N; i += L) {
     typename Bits<L>::type b;
     __builtin_memcpy(&b, &v[i], 2 * L);
-    *reinterpret_cast<typename Bits<L>::type *>(p + i) = b;
+    auto *to = reinterpret_cast<typename Bits<L>::type *>(p + i);
+    if constexpr (PAST) __builtin_nontemporal_store(b, to);
+    else *to = b;
   }
 }
 
@@ -63,10 +68,9 @@ __device__ __forceinline__ void store_bits(uint16_t *p, const uint16_t (&v)[N]) 
 // place.  The angle of pair i at position p is kept as a fraction of a turn in 64 bits, p * steps[i] mod 2^64, so that a far
 // position loses nothing; its upper half goes on.  A workgroup puts the cosines and sines of its rows into LDS, once for all heads; then its lanes
 // take units of VEC pairs (half: two loads of VEC values, interleaved: one of twice as many), all heads of all its rows in turn.  Bound by
-// memory: 64 987 rows of 32 heads of 128, 533 MB read and as many written in 180 us, 5.9 TB/s; few rows are one chain of position, angle, cosine
-// and load, 3 us.  Loads and stores past the caches: 65 536 rows of 32 heads 190 -> 167 us, but of 40 interleaved ones of 80 167 -> 264 and
-// of 10 of 64 25.6 -> 33.2 (stores alone 181, 228, 30.7); and what follows reads the keys from the caches.
-template <int VEC, int L, bool HALF>
+// memory: 64 987 rows of 32 heads of 128, 533 MB read and as many written in 168 us, 6.3 TB/s; few rows are one chain of position, angle, cosine
+// and load, 3 us.  PAST: past the caches.
+template <int VEC, int L, bool HALF, bool PAST>
 __global__ __launch_bounds__(256) void rotary_kernel(const int32_t *positions, int rows, int per_block, RotaryArgs a) {
   extern __shared__ float lds_turn[];                     // cosines [per_block, pairs], sines
   const int first = blockIdx.x * per_block, count = min(per_block, rows - first), pairs = a.pairs;
@@ -90,13 +94,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(const int32_t *positions, i
     const int from = (key ? h - a.n_heads : h) * a.head_dim;
     const uint16_t *in = (key ? a.k.in + at * a.k.in_stride : a.q.in + at * a.q.in_stride) + from;
     uint16_t *out = (key ? a.k.out + at * a.k.out_stride : a.q.out + at * a.q.out_stride) + from;
-    if (u >= turning) {
-      uint16_t v[2 * VEC];
-      load_bits<L>(in + 2 * VEC * u, v);
-      store_bits<L>(out + 2 * VEC * u, v);
-      continue;
-    }
-    const float *c = lds_cos + row * pairs + VEC * u, *s = lds_sin + row * pairs + VEC * u;
+    // (units that are copied take the same loads and stores as those that are turned)
+    const bool turns = u < turning;
+    const float *c = lds_cos + row * pairs + VEC * (turns ? u : 0), *s = lds_sin + row * pairs + VEC * (turns ? u : 0);
     const auto pair = [&](uint16_t &x, uint16_t &y, int e) {
       const float fx = bf16_to_f32(x), fy = bf16_to_f32(y);
       const uint32_t two = cvt_pk_bf16(fmaf(fx, c[e], -(fy * s[e])), fmaf(fy, c[e], fx * s[e]));
@@ -104,19 +104,24 @@ __global__ __launch_bounds__(256) void rotary_kernel(const int32_t *positions, i
       y = (uint16_t)(two >> 16);
     };
     if constexpr (HALF) {
+      const int at0 = turns ? VEC * u : pairs + VEC * u, at1 = turns ? pairs + VEC * u : a.head_dim / 2 + VEC * u;
       uint16_t x[VEC], y[VEC];
-      load_bits<L>(in + VEC * u, x);
-      load_bits<L>(in + pairs + VEC * u, y);
+      load_bits<L, PAST>(in + at0, x);
+      load_bits<L, PAST>(in + at1, y);
+      if (turns) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) pair(x[e], y[e], e);
-      store_bits<L>(out + VEC * u, x);
-      store_bits<L>(out + pairs + VEC * u, y);
+        for (int e = 0; e < VEC; ++e) pair(x[e], y[e], e);
+      }
+      store_bits<L, PAST>(out + at0, x);
+      store_bits<L, PAST>(out + at1, y);
     } else {
       uint16_t v[2 * VEC];
-      load_bits<L>(in + 2 * VEC * u, v);
+      load_bits<L, PAST>(in + 2 * VEC * u, v);
+      if (turns) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) pair(v[2 * e], v[2 * e + 1], e);
-      store_bits<L>(out + 2 * VEC * u, v);
+        for (int e = 0; e < VEC; ++e) pair(v[2 * e], v[2 * e + 1], e);
+      }
+      store_bits<L, PAST>(out + 2 * VEC * u, v);
     }
   }
 }
@@ -159,7 +164,7 @@ static bool overlap(Span x, Span y, int rows) {
 
 static constexpr int kMaxHead = 512;                      // (a unit of two values a lane: a head is at most one workgroup)
 // A launch takes fewer than 2^32 lanes, 256 a workgroup of up to 8 rows.
-static constexpr int kMaxRows = 8 * ((1 << 24) - 1);
+static constexpr int kMaxBlocks = (1 << 24) - 1, kMaxRows = 8 * kMaxBlocks;
 
 }  // namespace et
 
@@ -244,7 +249,8 @@ int et_rotary_apply(const et_rotary *rotary, const int32_t *positions_dev, int32
   // sharing one: us at one / 2 / 4 / 8 rows of 32 heads of 128 (256 units), 65 536 rows 191 / 193 / 197 / 205, 300 rows 3.1 / 3.3 / 4.0 / 5.8; of 40
   // interleaved heads of 80 (400 units) 168 / 174 / 194 / 218; but of 5 heads of 64 (20 units) 46.8 / 26.0 / 19.4 / 14.9.  With fewer than
   // one unit a lane instead: 65 536 rows of 4 heads of 80 in units of 4 (80 units) 21.3 -> 27.1, of 16 heads of 64 39.4 -> 41.0.
-  const int per_block = std::max(1, std::min({8, rows / 512, 511 / (heads * a.units)}));
+  const int least = (rows + kMaxBlocks - 1) / kMaxBlocks;
+  const int per_block = std::max({1, least, std::min({8, rows / 512, 511 / (heads * a.units)})});
   const unsigned blocks = (unsigned)((rows + per_block - 1) / per_block);
   const size_t lds = (size_t)per_block * pairs * 2 * sizeof(float);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -253,11 +259,21 @@ int et_rotary_apply(const et_rotary *rotary, const int32_t *positions_dev, int32
     ET_LAUNCH_CHECK();
     return ET_OK;
   };
+  // Past the caches where what is read and written exceeds the memory side's (256 MB) anyway, and every store writes whole lines of 128 bytes: runs of
+  // dimensions that lie together are half of rot_dim and of a head's rest (half), the whole row, or, in place, rot_dim (interleaved).  us cached / past:
+  // 64 987 rows of 32 heads of 128 191 / 168, 40 interleaved ones of 80, 32 dimensions turned, 147 / 139; 16 000 rows of 32 (131 MB each way)
+  // 46.4 / 43.2, again and again on the same rows 41.2 / 42.6; 4000 rows 12.1 / 13.3; 64 987 of 10 of 128, 64 turned (runs of 64 bytes), 64.6 / 69.8.
+  const int run = half ? pairs | r.head_dim | (in_place ? 0 : (r.head_dim - r.rot_dim) / 2) : in_place && r.rot_dim < r.head_dim ? r.rot_dim | r.head_dim : 0;
+  bool past = run % 64 == 0 && (int64_t)rows * heads * a.units * vec * 4 >= 128 << 20;
+  for (const et_rotary_rows *x : {q, &kr})
+    past = past && (x->n_heads == 0 || ((uintptr_t)x->out_dev % 128 == 0 && x->out_stride % 64 == 0 && (int64_t)x->n_heads * r.head_dim % 64 == 0));
   switch (load) {
-    case 8: return launch(half ? rotary_kernel<8, 8, true> : rotary_kernel<4, 8, false>);
-    case 4: return launch(half ? rotary_kernel<4, 4, true> : rotary_kernel<2, 4, false>);
-    case 2: return launch(half ? rotary_kernel<2, 2, true> : rotary_kernel<1, 2, false>);
-    default: return launch(half ? rotary_kernel<1, 1, true> : rotary_kernel<1, 1, false>);
+    case 8:
+      if (past) return launch(half ? rotary_kernel<8, 8, true, true> : rotary_kernel<4, 8, false, true>);
+      return launch(half ? rotary_kernel<8, 8, true, false> : rotary_kernel<4, 8, false, false>);
+    case 4: return launch(half ? rotary_kernel<4, 4, true, false> : rotary_kernel<2, 4, false, false>);
+    case 2: return launch(half ? rotary_kernel<2, 2, true, false> : rotary_kernel<1, 2, false, false>);
+    default: return launch(half ? rotary_kernel<1, 1, true, false> : rotary_kernel<1, 1, false, false>);
   }
 }
 

@@ -164,12 +164,12 @@ def test_rotary_launches_what_it_accepts(ask):
 def test_resize_launches_what_it_accepts(ask):
     """One launch for a step; for thousands of rows a second one where the new state takes the old one's place; two beyond 4096 sequences."""
     for seqs in (0, 1, 256, 1024, 1025, 4096, 4097, 2 ** 20, 2 ** 20 + 1):
-        for rows in (0, 1, 2048, 2049, 10 ** 6, 2 ** 31 - 1):
+        for rows in (0, 1, 1024, 1025, 6144, 6145, 10 ** 6, 2 ** 31 - 1):
             for apart in (0, 1):
                 (code, lanes, launches, _, _, bytes), = ask([("resize", seqs, 3, rows, apart)])
                 if seqs > 2 ** 20:
                     assert code == -1 and launches == 0
                     continue
-                several = max(rows, seqs) > 2048
+                several = max(rows, seqs) > 6144
                 assert code == 0 and 0 < lanes < 2 ** 32 and (bytes > 0) == (seqs > 4096)
                 assert launches == (2 if seqs > 4096 or (several and not apart) else 1), (seqs, rows, apart)

@@ -201,3 +201,20 @@ def test_columns_of_one_matrix():
             r.apply(a, b, pos, out=out)
     both = r.apply(q, q, pos)                             # one tensor as both is fine where nothing of it is written
     assert torch.equal(both[0], both[1])
+
+
+@pytest.mark.parametrize("layout,heads,kv,d,rot,in_place", [("half", 14, 2, 128, 128, False), ("interleaved", 14, 2, 128, 64, False), ("interleaved", 32, 0, 64, 64, True),
+                                                            ("half", 12, 4, 256, 128, True), ("interleaved", 23, 2, 80, 32, False)])
+def test_large_calls_equal_small_ones(layout, heads, kv, d, rot, in_place):
+    """More than the caches hold (134 MB written), against the same rows a thousand at a time."""
+    rows = 2 ** 26 // ((heads + kv) * d) + 77
+    g = torch.Generator("cuda:0").manual_seed(6)
+    q, k = (torch.randn((rows, n * d), generator=g, device="cuda:0").to(torch.bfloat16) if n else None for n in (heads, kv))
+    pos = torch.randint(-2 ** 31, 2 ** 31, (rows,), generator=g, device="cuda:0").int()
+    r = et.Rotary(d, rot, layout=layout)
+    want = [], []
+    for i in range(0, rows, 1000):
+        for w, x in zip(want, r.apply(q[i:i + 1000], None if k is None else k[i:i + 1000], pos[i:i + 1000])):
+            w.append(x)
+    got = r.apply(q, k, pos, out=(q, k) if in_place else None)
+    assert torch.equal(got[0], torch.cat(want[0])) and (k is None or torch.equal(got[1], torch.cat(want[1])))
