@@ -191,15 +191,15 @@ __device__ __forceinline__ uint32_t mx_encode8(u32x4 x, uint32_t exponent) {
 // the way to a place is a chain of four loads, so rows share it when there are many.  What is read or written once in long
 // streams (new rows, unquantised cells, rows read back) goes past the caches: 391 MB of e4m3 codes read back 265 -> 254 us, 130 000
 // rows of 4 heads of 80 73 -> 65, 134 MB of bfloat16 rows stored 110 -> 101; codes and the cells of a read do not gain by it.
-// SLOTS: the rows' places are given, in the place of `cu`.  In 4 bits 65 500 rows of 16 heads of 96 are stored in 105 us and read back in 77: 403 MB of
-// rows and 107 of codes and exponents each way, which is what passes the memory side (403 + 111 MB, 5.7 TB/s for both).
+// SLOTS: the rows' places are given, in the place of `cu`.  In 4 bits 65 500 rows of 16 heads of 96 are stored in 105 us and read back in 73: 403 MB of
+// rows and 107 of codes and exponents each way, which is what passes the memory side (403 + 111 MB, 5.8 TB/s for both).
 constexpr int kBatch = 4;
 template <int HD, int FMT, bool STORE, bool SLOTS>
 __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const int32_t *len, const int32_t *table, int n_seqs, int rows,
                                                       int per_block, int table_stride, int pages_per_seq, int page_shift, KvPages c,
                                                       uint16_t *k, int64_t k_stride, uint16_t *v, int64_t v_stride) {
   using Lay = KvLayout<HD, FMT>;
-  constexpr int LANES = kv_lanes<HD>(), GROUPS = 256 / LANES;
+  constexpr int UNITS = FMT == ET_KV_MXFP4 && HD % 128 == 0 ? 2 : 1, LANES = kv_lanes<HD>() / UNITS, GROUPS = 256 / LANES;
   __shared__ int4 lds_place[64];                         // byte offset of the page (two words), token of the page, 0 / 1 / 2
   // In 4 bits neighbouring workgroups' rows share cache lines of exponents.  An XCD takes 32 neighbours, so that they meet in its cache: 65 500 rows of
   // 16 heads of 96 stored and read back 203 -> 182 us, 32 800 of 32 of 80 201 -> 165, others level (8 neighbours 186, 170; an eighth of
@@ -221,77 +221,125 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const i
   int token = threadIdx.x / LANES / heads2, j = threadIdx.x / LANES % heads2;
   const bool in_row = sub * 8 < HD;
   __syncthreads();
-  auto turns = [&](auto batch) {
-    constexpr int N = decltype(batch)::value;
-    u32x4 x[N];
-    uint2 codes[N];
-    uint16_t top[N];                                     // in 4 bits: the block's exponent
-    uint16_t *row[N];
-    char *cell[N], *top_at[N];
-    int go[N];                                           // 0: nothing to do, 1: no place in the cache, 2: a place
+  if constexpr (FMT == ET_KV_MXFP4) {
+    // Where a row is whole lines of 128 bytes twice over, a lane has two times eight values, LANES * 8 apart, for one way to them: 4999 rows of 4 heads of
+    // 128 stored and read back 11.0 -> 9.8 us, 90 000 of one of 256 89 -> 84, 131 000 of 8 of 128 117 -> 119 (elsewhere stores of parts of
+    // lines: 65 500 of 16 of 96 181 -> 223).
+    auto turns = [&](auto batch) {
+      constexpr int N = decltype(batch)::value;
+      u32x4 x[N][UNITS];
+      uint32_t codes[N][UNITS], top[N][UNITS];
+      uint16_t *row[N];
+      char *cell[N], *top_at[N];
+      int go[N], next[N];                                  // (0: nothing to do, 1: no place in the cache, 2: a place; bytes to the other exponent)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int4 place = lds_place[min(token, 63)];
-      go[i] = token < count ? place.w : 0;
-      const bool value = j >= c.kv_heads;
-      const int h = value ? j - c.kv_heads : j;
-      row[i] = (value ? v + (first + (int64_t)token) * v_stride : k + (first + (int64_t)token) * k_stride) + h * HD + sub * 8;
-      char *page = c.data + (int64_t)((uint64_t)(uint32_t)place.y << 32 | (uint32_t)place.x);
-      const uint32_t head = (uint32_t)h * head_bytes;
-      cell[i] = page + (head + (value ? Lay::values(n) : 0) + place.z * Lay::kRow + sub * Lay::kEight);
-      if constexpr (FMT == ET_KV_MXFP4) {
-        const int block = min(sub / (kMxBlock / 8), Lay::kBlocks - 1);
-        top_at[i] = page + (head + (value ? Lay::value_scale(n) + block * n + place.z : Lay::key_scale(n) + place.z * Lay::kBlocks + block));
-      } else {
-        top_at[i] = page + (head + (value ? Lay::value_scale(n) : Lay::key_scale(n)) + place.z * 2);
+      for (int i = 0; i < N; ++i) {
+        const int4 place = lds_place[min(token, 63)];
+        go[i] = token < count ? place.w : 0;
+        const bool value = j >= c.kv_heads;
+        const int h = value ? j - c.kv_heads : j, block = sub / 4;
+        row[i] = (value ? v + (first + (int64_t)token) * v_stride : k + (first + (int64_t)token) * k_stride) + h * HD + sub * 8;
+        char *head = c.data + (int64_t)((uint64_t)(uint32_t)place.y << 32 | (uint32_t)place.x) + (uint32_t)h * head_bytes;
+        cell[i] = head + ((value ? Lay::values(n) : 0) + place.z * Lay::kRow + sub * 4);
+        top_at[i] = head + (value ? Lay::value_scale(n) + block * n + place.z : Lay::key_scale(n) + place.z * Lay::kBlocks + block);
+        next[i] = LANES / 4 * (value ? n : 1);
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+          x[i][u] = u32x4{0, 0, 0, 0};
+          codes[i][u] = top[i][u] = 0;
+          if (go[i] == 2 && in_row) {
+            if constexpr (STORE) {
+              x[i][u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(row[i] + u * LANES * 8));
+            } else {
+              codes[i][u] = *reinterpret_cast<const uint32_t *>(cell[i] + u * LANES * 4);
+              top[i][u] = *reinterpret_cast<const uint8_t *>(top_at[i] + u * next[i]);
+            }
+          }
+        }
+        token += skip;
+        j += over;
+        if (j >= heads2) j -= heads2, ++token;
       }
-      x[i] = u32x4{0, 0, 0, 0};
-      codes[i] = make_uint2(0, 0);
-      top[i] = 0;
-      if (go[i] == 2 && in_row) {
-        if constexpr (STORE) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(row[i]));
-        else if constexpr (FMT == ET_KV_BF16) x[i] = *reinterpret_cast<const u32x4 *>(cell[i]);
-        else if constexpr (FMT == ET_KV_MXFP4) {
-          codes[i].x = *reinterpret_cast<const uint32_t *>(cell[i]);
-          top[i] = *reinterpret_cast<const uint8_t *>(top_at[i]);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+          if constexpr (STORE) {
+            uint32_t most = magnitude8(x[i][u]);
+            most = dpp_max<0x4E>(dpp_max<0xB1>(most));
+            const bool number = most < 0x7F80u;
+            const uint32_t exponent = number ? mx_exponent(most) : 255u, code = number ? mx_encode8(x[i][u], exponent) : 0u;
+            if (go[i] == 2 && in_row) {
+              *reinterpret_cast<uint32_t *>(cell[i] + u * LANES * 4) = code;
+              if (sub % 4 == 0) *reinterpret_cast<uint8_t *>(top_at[i] + u * next[i]) = (uint8_t)exponent;
+            }
+          } else {
+            if (go[i] && in_row)
+              __builtin_nontemporal_store(mx_decode8(codes[i][u], top[i][u]), reinterpret_cast<u32x4 *>(row[i] + u * LANES * 8));
+          }
+        }
+    };
+    constexpr int BATCH = kBatch / UNITS;
+    int left = (count * heads2 + GROUPS - 1) / GROUPS;
+    for (; left >= BATCH; left -= BATCH) turns(std::integral_constant<int, BATCH>());
+    for (; left > 0; --left) turns(std::integral_constant<int, 1>());
+  } else {
+    auto turns = [&](auto batch) {
+      constexpr int N = decltype(batch)::value;
+      u32x4 x[N];
+      uint2 codes[N];
+      uint16_t top[N];
+      uint16_t *row[N];
+      char *cell[N], *top_at[N];
+      int go[N];                                           // 0: nothing to do, 1: no place in the cache, 2: a place
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int4 place = lds_place[min(token, 63)];
+        go[i] = token < count ? place.w : 0;
+        const bool value = j >= c.kv_heads;
+        const int h = value ? j - c.kv_heads : j;
+        row[i] = (value ? v + (first + (int64_t)token) * v_stride : k + (first + (int64_t)token) * k_stride) + h * HD + sub * 8;
+        char *page = c.data + (int64_t)((uint64_t)(uint32_t)place.y << 32 | (uint32_t)place.x);
+        const uint32_t head = (uint32_t)h * head_bytes;
+        cell[i] = page + (head + (value ? Lay::values(n) : 0) + place.z * Lay::kRow + sub * Lay::kEight);
+        top_at[i] = page + (head + (value ? Lay::value_scale(n) : Lay::key_scale(n)) + place.z * 2);
+        x[i] = u32x4{0, 0, 0, 0};
+        codes[i] = make_uint2(0, 0);
+        top[i] = 0;
+        if (go[i] == 2 && in_row) {
+          if constexpr (STORE) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(row[i]));
+          else if constexpr (FMT == ET_KV_BF16) x[i] = *reinterpret_cast<const u32x4 *>(cell[i]);
+          else {
+            codes[i] = *reinterpret_cast<const uint2 *>(cell[i]);
+            top[i] = *reinterpret_cast<const uint16_t *>(top_at[i]);
+          }
+        }
+        token += skip;
+        j += over;
+        if (j >= heads2) j -= heads2, ++token;
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if constexpr (STORE && FMT != ET_KV_BF16) {
+          uint32_t most = magnitude8(x[i]);
+          most = group_max<LANES>(most);
+          const bool number = most - 1u < 0x7F7Fu;          // neither 0 nor without end
+          codes[i] = quantise8<FMT>(x[i], number ? most : 0x3F80u);
+          if (most >= 0x7F80u) most = 0x7FC0u, codes[i] = make_uint2(0, 0);
+          if (go[i] == 2 && in_row) *reinterpret_cast<uint2 *>(cell[i]) = codes[i];
+          if (go[i] == 2 && sub == 0) *reinterpret_cast<uint16_t *>(top_at[i]) = (uint16_t)most;
+        } else if constexpr (STORE) {
+          if (go[i] == 2 && in_row) __builtin_nontemporal_store(x[i], reinterpret_cast<u32x4 *>(cell[i]));
         } else {
-          codes[i] = *reinterpret_cast<const uint2 *>(cell[i]);
-          top[i] = *reinterpret_cast<const uint16_t *>(top_at[i]);
+          if constexpr (FMT != ET_KV_BF16) x[i] = dequantise8<FMT>(codes[i], kv_factor<FMT>(top[i]));
+          if (go[i] && in_row) __builtin_nontemporal_store(x[i], reinterpret_cast<u32x4 *>(row[i]));
         }
       }
-      token += skip;
-      j += over;
-      if (j >= heads2) j -= heads2, ++token;
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if constexpr (STORE && FMT == ET_KV_MXFP4) {
-        uint32_t most = magnitude8(x[i]);
-        most = dpp_max<0x4E>(dpp_max<0xB1>(most));        // four lanes' values are a block
-        const bool number = most < 0x7F80u;
-        const uint32_t exponent = number ? mx_exponent(most) : 255u, code = number ? mx_encode8(x[i], exponent) : 0u;
-        if (go[i] == 2 && in_row) *reinterpret_cast<uint32_t *>(cell[i]) = code;
-        if (go[i] == 2 && in_row && sub % 4 == 0) *reinterpret_cast<uint8_t *>(top_at[i]) = (uint8_t)exponent;
-      } else if constexpr (STORE && FMT != ET_KV_BF16) {
-        uint32_t most = magnitude8(x[i]);
-        most = group_max<LANES>(most);
-        const bool number = most - 1u < 0x7F7Fu;          // neither 0 nor without end
-        codes[i] = quantise8<FMT>(x[i], number ? most : 0x3F80u);
-        if (most >= 0x7F80u) most = 0x7FC0u, codes[i] = make_uint2(0, 0);
-        if (go[i] == 2 && in_row) *reinterpret_cast<uint2 *>(cell[i]) = codes[i];
-        if (go[i] == 2 && sub == 0) *reinterpret_cast<uint16_t *>(top_at[i]) = (uint16_t)most;
-      } else if constexpr (STORE) {
-        if (go[i] == 2 && in_row) __builtin_nontemporal_store(x[i], reinterpret_cast<u32x4 *>(cell[i]));
-      } else {
-        if constexpr (FMT == ET_KV_MXFP4) x[i] = mx_decode8(codes[i].x, top[i]);
-        else if constexpr (FMT != ET_KV_BF16) x[i] = dequantise8<FMT>(codes[i], kv_factor<FMT>(top[i]));
-        if (go[i] && in_row) __builtin_nontemporal_store(x[i], reinterpret_cast<u32x4 *>(row[i]));
-      }
-    }
-  };
-  int left = (count * heads2 + GROUPS - 1) / GROUPS;
-  for (; left >= kBatch; left -= kBatch) turns(std::integral_constant<int, kBatch>());
-  for (; left > 0; --left) turns(std::integral_constant<int, 1>());
+    };
+    int left = (count * heads2 + GROUPS - 1) / GROUPS;
+    for (; left >= kBatch; left -= kBatch) turns(std::integral_constant<int, kBatch>());
+    for (; left > 0; --left) turns(std::integral_constant<int, 1>());
+  }
 }
 
 static bool kv_format(int format) { return (format >= ET_KV_BF16 && format <= ET_KV_INT8) || format == ET_KV_MXFP4; }
@@ -349,9 +397,9 @@ static int check_rows(const et_kv_cache *cache, const et_kv_seqs *seqs, const in
 // 128 stored 116 / 110 / 112 / 118 / 118, e4m3 stored and read back 251 / 190 / 177 / 175 / 178; 130 000 bfloat16 rows of 4 heads of 80
 // read 179 / 93 / 73 / 72 / 77; 5000 int8 rows of 4 heads of 128 stored and read back 17.7 / 12.9 / 15.1 / 19.0 / 26.7; at 16 / 32 / 64
 // rows: 928 000 int8 rows of 3 heads of 64 read 293 / 261 / 251, 630 000 of one head of 128 stored and read back 259 / 222 / 220.
-// In 4 bits four turns too, or eight where those are fewer than four rows; stored and read back at 4 / 8 / 16 turns: 16 000 rows of 4 heads of 128
-// 18.8 / 21.2 / 21.2, 131 000 of 8 118 / 122 / 126, 180 000 of 4 of 64 88 / 91 / 101; 65 500 of 16 of 96 193 / 182 / 189, 32 800 of 32 of 80
-// 181 / 165 / 174.
+// In 4 bits four turns (of eight values a lane) too, or eight where those are fewer than four rows; stored and read back at 4 / 8 / 16 turns: 16 000 rows
+// of 4 heads of 128 19.3 / 21.4 / 21.2, 131 000 of 8 119 / 130 / 126, 180 000 of 4 of 64 85 / 90 / 101; 65 500 of 16 of 96 193 / 182 / 189,
+// 32 800 of 32 of 80 181 / 165 / 174.  Half or twice as many workgroups at the least: 4999 rows of 4 heads of 128 11.0 -> 11.6, 13.1.
 static int rows_per_block(int rows, const et_kv_cache &c) {
   const int lanes = c.head_dim <= 64 ? 8 : c.head_dim <= 128 ? 16 : 32;
   const auto turns = [&](int n) { return n * (256 / lanes) / (2 * c.n_kv_heads); };
