@@ -136,9 +136,10 @@ __device__ __forceinline__ int64_t slot_of(const PoolArgs &a, int page, int pos)
 
 // Up to 1024 PER sequences: every workgroup adds up all of them by itself, PER to a lane, and keeps the sums in LDS; then lanes take entries and
 // rows and look their sequence up there.  kFill: tables, positions, places and row ranges; kGive: pages given back and the new state, by one
-// workgroup.  Both in one for a decoding step (a single workgroup); otherwise the first of many gives and the others fill, or, where the new
-// state takes the old one's place, which the others read, a launch of its own gives.  The loads of a turn are issued together.
-// A step of 256 sequences is one workgroup's chain, 6.6 us: lengths, sums (two barriers), a search in LDS, table or ring, result.  A million
+// workgroup.  The first workgroup gives and the others fill; where the new state takes the old one's place, which the others read, one workgroup does both,
+// or a launch of its own gives.  The loads of a turn are issued together.
+// A step of 256 sequences, some of which end, is two workgroups' chains, 5.6 to 6.3 us (in one 6.9): lengths, sums (two barriers), a search in LDS,
+// table or ring, result.  A million
 // rows are written in 11 us, 12 bytes each: four such turns of 255 workgroups, one a compute unit (127 / 383 / 511 / 1023 workgroups 14.9 / 13.3 / 12.9 /
 // 17.2 us).  Two or four rows a lane and turn 12.2 / 14.2; 64 registers, so that a compute unit holds two workgroups, 13.0.
 constexpr int kGive = 1, kFill = 2;
@@ -334,12 +335,11 @@ int et_kv_resize(const et_kv_pool *pool, const int32_t *state_dev, int32_t *stat
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const PoolArgs a{pool->ring_dev, page_table_dev, kv_len_dev, new_len_dev, pool->n_pages, __builtin_ctz(page), table_stride, pages_per_seq, n_seqs};
   if (!need) {
-    // A turn of 1024 rows a workgroup, and one that gives; where the new state takes the old one's place, and the giving a launch of its own (3 us),
-    // one workgroup for everything up to six turns.  us, one / several: 4 sequences, 1544 rows 4.9 / 4.6; 256, 2634 7.0 / 5.1, in place 7.0 / 8.2; in
-    // place 4, 5516 7.3 / 7.8; 16, 8550 10.4 / 7.8; 4096, 4096 11.5 / 12.8.  With turns of 2048 rows 16 sequences, 62 605 rows 4.8 -> 5.7,
-    // 1000, 8000 5.7 -> 6.8.
-    const int turns = (int)(((int64_t)std::max(rows, n_seqs) + kPoolThreads - 1) / kPoolThreads), fillers = std::min(255, turns);
-    const bool one = turns <= (state_out_dev == state_dev ? 6 : 1), apart = !one && state_out_dev == state_dev;
+    // A turn of 1024 rows a workgroup, and one that gives; in place one workgroup for everything up to six turns, as the giving would be a launch of its own
+    // (3 us).  us, one / several: 256 sequences, 253 rows 6.9 / 5.6; 4, 1544 4.9 / 4.6; 256, 2634 7.0 / 5.1, in place 7.0 / 8.2; in place 4, 5516 7.3 / 7.8;
+    // 16, 8550 10.4 / 7.8; 4096, 4096 11.5 / 12.8.  With turns of 2048 rows 16 sequences, 62 605 rows 4.8 -> 5.7, 1000, 8000 5.7 -> 6.8.
+    const int turns = std::max(1, (int)(((int64_t)std::max(rows, n_seqs) + kPoolThreads - 1) / kPoolThreads)), fillers = std::min(255, turns);
+    const bool in_place = state_out_dev == state_dev, one = in_place && turns <= 6, apart = in_place && !one;
     auto launch = [&](int blocks, int what) {
       (n_seqs <= kPoolThreads ? pool_resize_kernel<1> : pool_resize_kernel<4>)<<<blocks, kPoolThreads, 0, stream>>>(
           state_dev, kv_len_dev, new_len_dev, rows, what, a, state_out_dev, cu_rows_dev, positions_dev, slots_dev);
