@@ -125,3 +125,32 @@ def test_errors_of_an_entry_point_carry_its_message():
         c.attend(randn(3, 128), tab, ln, 0)
     with pytest.raises(et.EtError, match="aligned"):
         c.append_at(randn(3, 130)[:, 2:], randn(3, 128), torch.zeros(3, dtype=torch.int64, device="cuda:0"))
+
+
+@pytest.mark.parametrize("rows", [0, 1, 3, 500, 9000])
+def test_results_of_a_call_keep_apart(rows):
+    """Small results share a piece of memory: aligned, apart, of their own shapes, and each survives the others."""
+    d, r = 64, et.Rotary(64)
+    g = torch.Generator("cuda:0").manual_seed(rows)
+    q, k = (torch.randn((rows, n * d), generator=g, device="cuda:0").to(torch.bfloat16) for n in (9, 3))
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda:0")
+    want = r.apply(q, None, pos)[0], r.apply(k, None, pos)[0]
+    a, b = r.apply(q, k, pos)
+    assert a.shape == q.shape and b.shape == k.shape and a.is_contiguous() and b.is_contiguous() and a.data_ptr() % 128 == b.data_ptr() % 128 == 0
+    assert not a.requires_grad and a._base is None and a.dtype is torch.bfloat16
+    keep = a.clone()
+    b.zero_()
+    del b
+    filler = [torch.full((64, d), 7.0, dtype=torch.bfloat16, device="cuda:0") for _ in range(64)]
+    assert torch.equal(a, keep) and torch.equal(a, want[0])
+    a, b = r.apply(q, k, pos)
+    del a, filler
+    assert torch.equal(b, want[1]) and torch.equal(b + b, want[1] + want[1])
+    pool = et.PagePool(700, 16)
+    table = torch.full((1, 700), -1, dtype=torch.int32, device="cuda:0")
+    old, new = torch.zeros(1, dtype=torch.int32, device="cuda:0"), torch.full((1,), rows, dtype=torch.int32, device="cuda:0")
+    cu, positions, slots = pool.resize(table, old, new, rows)
+    assert cu.dtype is positions.dtype is torch.int32 and slots.dtype is torch.int64
+    assert cu.tolist() == [0, rows] and torch.equal(positions, pos) and torch.equal(slots, pos.long())
+    positions.fill_(-5)
+    assert cu.tolist() == [0, rows] and torch.equal(slots, pos.long())
