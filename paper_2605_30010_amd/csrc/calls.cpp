@@ -183,7 +183,8 @@ CALL(read) {
   const int64_t rows = cu ? whole(arg[5], INT32_MAX) : seqs.s.n_seqs, width = (int64_t)cache->n_kv_heads * cache->head_dim;
   if (rows < 0) Py_RETURN_NONE;
   const int64_t shape[2] = {rows, width};
-  const auto [k, v] = fresh({{shape, at::kBFloat16}, {shape, at::kBFloat16}}, device);
+  const auto out = fresh({{shape, at::kBFloat16}, {shape, at::kBFloat16}}, device);
+  const at::Tensor &k = out[0], &v = out[1];
   return made(unlocked([&] {
                 return lib.read(cache, &seqs.s, cu ? static_cast<const int32_t *>(cu->data_ptr()) : nullptr, (int32_t)rows,
                                 static_cast<uint16_t *>(k.data_ptr()), width, static_cast<uint16_t *>(v.data_ptr()), width, stream_of(arg[6]));
@@ -226,7 +227,8 @@ CALL(resize) {
   const int64_t rows = whole(arg[7], INT32_MAX);
   if (!fresh_len || rows < 0) Py_RETURN_NONE;
   const int64_t ranges = (int64_t)seqs.s.n_seqs + 1;
-  const auto [cu, positions, slots] = fresh({{ranges, at::kInt}, {rows, at::kInt}, {rows, at::kLong}}, device);
+  const auto out = fresh({{ranges, at::kInt}, {rows, at::kInt}, {rows, at::kLong}}, device);
+  const at::Tensor &cu = out[0], &positions = out[1], &slots = out[2];
   const size_t need = lib.resize_bytes(seqs.s.n_seqs);
   at::Tensor ws;
   if (need) ws = fresh({(int64_t)need}, at::kByte, device);

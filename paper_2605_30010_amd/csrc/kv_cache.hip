@@ -417,8 +417,8 @@ static int launch_rows(const et_kv_cache &cache, const et_kv_seqs &seqs, const i
   auto launch = [&](auto hd, auto fmt) {
     (slots ? kv_rows_kernel<hd.value, fmt.value, STORE, STORE> : kv_rows_kernel<hd.value, fmt.value, STORE, false>)<<<
         (rows + per_block - 1) / per_block, 256, 0, stream>>>(
-        slots ? reinterpret_cast<const int32_t *>(slots) : cu, seqs.kv_len_dev, seqs.page_table_dev, seqs.n_seqs, rows, per_block, seqs.table_stride, seqs.pages_per_seq, c.page_shift, c,
-        k, k_stride, v, v_stride);
+        slots ? reinterpret_cast<const int32_t *>(slots) : cu, seqs.kv_len_dev, seqs.page_table_dev, seqs.n_seqs, rows, per_block,
+        seqs.table_stride, seqs.pages_per_seq, c.page_shift, c, k, k_stride, v, v_stride);
     ET_LAUNCH_CHECK();
     return ET_OK;
   };

@@ -240,7 +240,8 @@ int et_rotary_apply(const et_rotary *rotary, const int32_t *positions_dev, int32
   int load = half ? widest({pairs, (r.head_dim - r.rot_dim) / 2, r.head_dim}) : widest({r.rot_dim, r.head_dim});
   for (const et_rotary_rows *x : {q, &kr})
     if (x->n_heads)
-      load = std::min(load, widest({rows > 1 ? x->in_stride : 0, rows > 1 ? x->out_stride : 0, (int64_t)((uintptr_t)x->in_dev / 2), (int64_t)((uintptr_t)x->out_dev / 2)}));
+      load = std::min(load, widest({rows > 1 ? x->in_stride : 0, rows > 1 ? x->out_stride : 0, (int64_t)((uintptr_t)x->in_dev / 2),
+                                    (int64_t)((uintptr_t)x->out_dev / 2)}));
   const int vec = half ? load : std::max(1, load / 2);
   const bool in_place = (q->n_heads == 0 || q->in_dev == q->out_dev) && (kr.n_heads == 0 || kr.in_dev == kr.out_dev);
   RotaryArgs a{{q->in_dev, q->in_stride, q->out_dev, q->out_stride}, {kr.in_dev, kr.in_stride, kr.out_dev, kr.out_stride}, r.steps_dev, q->n_heads,
