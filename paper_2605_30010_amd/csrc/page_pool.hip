@@ -79,31 +79,37 @@ __device__ __forceinline__ int find_seq_all(const int *first, int from, int n_se
   }
   return from;
 }
-// Gives pages behind sequences' ends back: of all `total` entries the workgroup takes up to 4096 from `back` on, a wavefront up to 256
+// Gives pages behind sequences' ends back, in turns: of all `total` entries the workgroup takes up to 4096 from `back` on, a wavefront up to 256
 // neighbours (their sequences lie between the first one's and the last one's).  Those that are pages go behind the ring's `count` free ones and the
-// `given` before them, in order.
+// `given` before them, in order.  A turn's entries are on their way while the turn before is put into the ring.
+constexpr int kGiveTurn = 4 * kPoolThreads;
+__device__ __forceinline__ int given_each(int64_t back, int total) {        // entries of a wavefront
+  return 64 * (int)min((total - back + kPoolThreads - 1) / kPoolThreads, (int64_t)4);
+}
 template <typename NewLength>
-__device__ __forceinline__ void give_pages(const PoolArgs &a, PoolState st, const int *shrink_first, int64_t back, int total, NewLength new_of,
-                                           int &given, int (&lds)[kPoolWaves]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, room = a.n_pages - st.count;
-  const int each = 64 * (int)min((total - back + kPoolThreads - 1) / kPoolThreads, (int64_t)4);      // entries of a wavefront
+__device__ __forceinline__ void find_given(const PoolArgs &a, const int *shrink_first, int64_t back, int total, NewLength new_of, int (&page)[4]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, each = given_each(back, total);
   const int64_t k0 = back + wave * each;
-  int page[4], mine = 0;
-  uint64_t votes[4] = {};
+#pragma unroll
+  for (int u = 0; u < 4; ++u) page[u] = -1;
   if (k0 < total) {
     const int lo = find_seq_all(shrink_first, 0, a.n_seqs, (int)k0), hi = find_seq_all(shrink_first, lo, a.n_seqs, (int)min(k0 + each - 1, total - 1ll));
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int64_t k = k0 + u * 64 + lane;
-      page[u] = -1;
       if (k < min(k0 + each, (int64_t)total)) {
         const int b = find_seq(shrink_first, lo, hi, (int)k);
         page[u] = a.table[(int64_t)b * a.table_stride + a.pages(new_of(b)) + ((int)k - shrink_first[b])];
       }
     }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) mine += __popcll(votes[u] = __ballot(a.is_page(page[u])));
   }
+}
+__device__ __forceinline__ void put_given(const PoolArgs &a, PoolState st, const int (&page)[4], int &given, int (&lds)[kPoolWaves]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, room = a.n_pages - st.count;
+  uint64_t votes[4];
+  int mine = 0;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) mine += __popcll(votes[u] = __ballot(a.is_page(page[u])));
   if (lane == 0) lds[wave] = mine;
   __syncthreads();
   int at = given;
@@ -188,7 +194,9 @@ __global__ __launch_bounds__(kPoolThreads) void pool_resize_kernel(const int32_t
   // turn by turn, an entry and a row, and entries that are given back
   const int64_t stride = (int64_t)share * kPoolThreads;
   int64_t base = fills ? (int64_t)place * kPoolThreads : 0;
-  for (int64_t back = 0; base < max(n_rows, n_grow) || back < n_shrink; base += stride, back += 4 * kPoolThreads) {
+  int back_page[4] = {-1, -1, -1, -1};
+  if (n_shrink) find_given(a, shrink_first, 0, n_shrink, new_of, back_page);
+  for (int64_t back = 0; base < max(n_rows, n_grow) || back < n_shrink; base += stride, back += kGiveTurn) {
     const int64_t i = base + t;
     int fresh_page = -1, page = -1, pos = 0;
     int32_t *entry_at = nullptr;
@@ -204,7 +212,13 @@ __global__ __launch_bounds__(kPoolThreads) void pool_resize_kernel(const int32_t
       if (slots && entry < had) page = a.table[(int64_t)b * a.table_stride + entry];
       else if (slots && entry < a.pages_per_seq) page = taken_page(a, st, grow_first[b] + entry - had);
     }
-    if (back < n_shrink) give_pages(a, st, shrink_first, back, n_shrink, new_of, given, lds_given);
+    if (back < n_shrink) {
+      int next_page[4] = {-1, -1, -1, -1};
+      if (back + kGiveTurn < n_shrink) find_given(a, shrink_first, back + kGiveTurn, n_shrink, new_of, next_page);
+      put_given(a, st, back_page, given, lds_given);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) back_page[u] = next_page[u];
+    }
     if (entry_at) *entry_at = fresh_page;
     if (i < n_rows) {
       if (positions) positions[i] = pos;
@@ -247,8 +261,16 @@ __global__ __launch_bounds__(kPoolThreads) void pool_plan_kernel(const int32_t *
   __threadfence_block();
   __syncthreads();
   int given = 0;
-  for (int64_t back = 0; back < sum.shrink; back += 4 * kPoolThreads)
-    give_pages(a, st, shrink_first, back, sum.shrink, [&](int b) { return max(a.new_len[b], 0); }, given, lds_given);
+  const auto new_of = [&](int b) { return max(a.new_len[b], 0); };
+  int page[4] = {-1, -1, -1, -1};
+  if (sum.shrink) find_given(a, shrink_first, 0, sum.shrink, new_of, page);
+  for (int64_t back = 0; back < sum.shrink; back += kGiveTurn) {
+    int next[4] = {-1, -1, -1, -1};
+    if (back + kGiveTurn < sum.shrink) find_given(a, shrink_first, back + kGiveTurn, sum.shrink, new_of, next);
+    put_given(a, st, page, given, lds_given);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) page[u] = next[u];
+  }
   if (t == 0) {
     cu[a.n_seqs] = clipped(sum.rows);
     *reinterpret_cast<int4 *>(plan->state) = make_int4(st.head, st.count, 0, 0);
