@@ -439,7 +439,9 @@ int et_attention_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, const u
  * The new tokens of all sequences are consecutive rows, sequence by sequence: cu_rows [n_seqs + 1] their ranges (as et_kv_append takes
  * them, with new_len as lengths), positions [rows] the place of each in its sequence, slots [rows] page * page_size + place in the page, or -1
  * where there is no page (a missing one, or past pages_per_seq).  positions_dev and slots_dev may be NULL; `rows` is how many
- * rows they have: rows past that are not written, nor is what lies behind the last sequence's.  cu_rows stops at 2^31 - 1.
+ * rows they have, and may be a bound: rows past that are not written, and those behind the last sequence's get position 0 and slot -1, so
+ * that et_kv_append_slots stores nothing for them (pool->keep_rest = 1: they stay as they are, which may be places of an earlier
+ * call).  cu_rows stops at 2^31 - 1.
  * kv_len, new_len and everything else of the table stay as they are, and so do the ring's pages that were free: with another buffer as state_out_dev
  * (state_out_dev = state_dev is allowed) a call is taken back by going on with the old state and the old lengths, as when
  * pages are missing.  A page must be in one place, a table's live entry or a free cell of the ring; sequences that share pages are the
@@ -450,6 +452,7 @@ int et_attention_paged(const et_kv_cache *cache, const et_kv_seqs *seqs, const u
 typedef struct {
   int32_t *ring_dev;           /* [n_pages]                                                          */
   int32_t n_pages, page_size;  /* page_size 16, 32, 64, 128 or 256                                   */
+  int32_t keep_rest;           /* 1: rows behind the last sequence's stay as they are; 0 otherwise   */
 } et_kv_pool;
 size_t et_kv_resize_workspace_bytes(int32_t n_seqs);
 int et_kv_resize(const et_kv_pool *pool, const int32_t *state_dev, int32_t *state_out_dev, int32_t *page_table_dev,

@@ -68,7 +68,7 @@ class _KvSeqs(C.Structure):
 
 
 class _KvPool(C.Structure):
-    _fields_ = [("ring_dev", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32)]
+    _fields_ = [("ring_dev", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("keep_rest", C.c_int32)]
 
 
 class _RotaryScaling(C.Structure):
@@ -810,15 +810,16 @@ class PagePool(_OnDevice):
             raise ValueError("ring must have n_pages = %d values, state 4, on one device" % n_pages)
         self.ring, self.state, self.device = ring, state, ring.device
         self.n_pages, self.page_size, self._lib = int(n_pages), int(page_size), load_library()
-        self._pool = _KvPool(ring.data_ptr(), self.n_pages, self.page_size)
+        self._pool, self._keeping = (_KvPool(ring.data_ptr(), self.n_pages, self.page_size, keep) for keep in (0, 1))
         self._calls, self._at, self._index = _calls, C.addressof(self._pool), self._number()
 
     def resize(self, page_table, kv_len, new_len, rows, state_out=None, out=None, stream=None):
         """Takes every sequence from kv_len to new_len tokens (int32 [n_seqs] each): its row of page_table (int32 [n_seqs, pages], rows may
         be strided) gets pages from the pool, or gives back those that it no longer needs.  Returns (cu_rows int32 [n_seqs + 1], positions
-        int32 [rows], slots int64 [rows]) of the new tokens, sequence by sequence; `rows` is how many there are, as the caller knows, or a bound
-        (rows behind the last sequence's hold anything, or stay as `out`, the same three, has them).  The pool's state is changed in
-        place, or goes to state_out int32 [4]: then the call is taken back by going on with the old state and lengths."""
+        int32 [rows], slots int64 [rows]) of the new tokens, sequence by sequence; `rows` is how many there are, as the caller knows, or a bound:
+        rows behind the last sequence's have position 0 and slot -1, for which KVCache.append_at stores nothing.  With `out`, the same three, they
+        stay as `out` has them (slots of an earlier call are places still: fill them with -1 before append_at gets them).  The pool's state is changed
+        in place, or goes to state_out int32 [4]: then the call is taken back by going on with the old state and lengths."""
         s = self._here(stream)
         if s is None:
             with self._elsewhere(stream):
@@ -844,6 +845,7 @@ class PagePool(_OnDevice):
         rows = int(rows)
         if rows < 0 or rows > _INT_MAX:
             raise ValueError("rows = %d must be in [0, 2^31 - 1]" % rows)
+        pool = self._pool if out is None else self._keeping
         if out is None:
             out = cu, positions, slots = kv_len.new_empty(n + 1), kv_len.new_empty(rows), kv_len.new_empty(rows, dtype=torch.int64)
         else:
@@ -855,7 +857,7 @@ class PagePool(_OnDevice):
         lib = self._lib
         need = lib.et_kv_resize_workspace_bytes(n) if n > 4096 else 0                # (none up to 4096 sequences)
         ws = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-        _check(lib.et_kv_resize(self._pool, self.state.data_ptr(), state_out.data_ptr(), page_table.data_ptr(), strides[0] if n > 1 else pages,
+        _check(lib.et_kv_resize(pool, self.state.data_ptr(), state_out.data_ptr(), page_table.data_ptr(), strides[0] if n > 1 else pages,
                                 pages, kv_len.data_ptr(), new_len.data_ptr(), n, rows, cu.data_ptr(), positions.data_ptr(),
                                 slots.data_ptr(), ws.data_ptr() if need else None, need, s))
         return out

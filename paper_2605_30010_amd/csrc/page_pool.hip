@@ -141,14 +141,14 @@ __device__ __forceinline__ int64_t slot_of(const PoolArgs &a, int page, int pos)
 }
 
 // Up to 1024 PER sequences: every workgroup adds up all of them by itself, PER to a lane, and keeps the sums in LDS; then lanes take entries and
-// rows and look their sequence up there.  kFill: tables, positions, places and row ranges; kGive: pages given back and the new state, by one
-// workgroup.  The first workgroup gives and the others fill; where the new state takes the old one's place, which the others read, one workgroup does both,
-// or a launch of its own gives.  The loads of a turn are issued together.
+// rows and look their sequence up there.  kFill: tables, positions, places and row ranges (kRest: of all `rows`, also those behind the last sequence's);
+// kGive: pages given back and the new state, by one workgroup.  The first workgroup gives and the others fill; where the new state takes the old
+// one's place, which the others read, one workgroup does both, or a launch of its own gives.  The loads of a turn are issued together.
 // A step of 256 sequences, some of which end, is two workgroups' chains, 5.5 to 6.1 us (in one 6.9): lengths, sums (two barriers), a search in LDS,
 // table or ring, result.  A million
 // rows are written in 11 us, 12 bytes each: four such turns of 255 workgroups, one a compute unit (127 / 383 / 511 / 1023 workgroups 14.9 / 13.3 / 12.9 /
 // 17.2 us).  Two or four rows a lane and turn 12.2 / 14.2; 64 registers, so that a compute unit holds two workgroups, 13.0.
-constexpr int kGive = 1, kFill = 2;
+constexpr int kGive = 1, kFill = 2, kRest = 4;
 template <int PER>
 __global__ __launch_bounds__(kPoolThreads) void pool_resize_kernel(const int32_t *state, const int32_t *len, const int32_t *new_len, int rows,
                                                                   int what, PoolArgs a, int32_t *state_out, int32_t *cu, int32_t *positions,
@@ -189,6 +189,7 @@ __global__ __launch_bounds__(kPoolThreads) void pool_resize_kernel(const int32_t
   const auto new_of = [&](int b) { return PER == 1 ? lds_len[b].y : max(new_len[b], 0); };
   const int last = a.n_seqs - 1;
   const int n_rows = fills && (positions || slots) ? (int)min((int64_t)rows, total.rows) : 0, n_grow = fills ? total.grow : 0;
+  const int n_all = fills && (positions || slots) && (what & kRest) ? rows : n_rows;
   const int n_shrink = gives ? total.shrink : 0;
   int given = 0;
   // turn by turn, an entry and a row, and entries that are given back
@@ -196,7 +197,7 @@ __global__ __launch_bounds__(kPoolThreads) void pool_resize_kernel(const int32_t
   int64_t base = fills ? (int64_t)place * kPoolThreads : 0;
   int back_page[4] = {-1, -1, -1, -1};
   if (n_shrink) find_given(a, shrink_first, 0, n_shrink, new_of, back_page);
-  for (int64_t back = 0; base < max(n_rows, n_grow) || back < n_shrink; base += stride, back += kGiveTurn) {
+  for (int64_t back = 0; base < max(n_all, n_grow) || back < n_shrink; base += stride, back += kGiveTurn) {
     const int64_t i = base + t;
     int fresh_page = -1, page = -1, pos = 0;
     int32_t *entry_at = nullptr;
@@ -220,7 +221,7 @@ __global__ __launch_bounds__(kPoolThreads) void pool_resize_kernel(const int32_t
       for (int u = 0; u < 4; ++u) back_page[u] = next_page[u];
     }
     if (entry_at) *entry_at = fresh_page;
-    if (i < n_rows) {
+    if (i < n_all) {
       if (positions) positions[i] = pos;
       if (slots) slots[i] = slot_of(a, page, pos);
     }
@@ -286,8 +287,8 @@ __device__ __forceinline__ int find_seq_wave(const int *first, int n_seqs, int x
   const int lo = find_seq_all(first, 0, n_seqs, x0);
   return find_seq(first, lo, find_seq_all(first, lo, n_seqs, x1), min(x, x1));
 }
-__global__ __launch_bounds__(256) void pool_fill_kernel(PoolArgs a, const int32_t *cu, PoolPlan *plan, int rows, int row_blocks, int32_t *positions,
-                                                        int64_t *slots) {
+__global__ __launch_bounds__(256) void pool_fill_kernel(PoolArgs a, const int32_t *cu, PoolPlan *plan, int rows, int rest, int row_blocks,
+                                                        int32_t *positions, int64_t *slots) {
   const PoolState st(plan->state, a.n_pages);
   const int32_t *grow_first = plan->grow_first();
   if ((int)blockIdx.x >= row_blocks) {                   // entries
@@ -299,18 +300,23 @@ __global__ __launch_bounds__(256) void pool_fill_kernel(PoolArgs a, const int32_
     }
     return;
   }
-  const int n = min(rows, plan->rows);
-  for (int64_t i0 = (int64_t)blockIdx.x * 256 + (threadIdx.x & ~63); i0 < n; i0 += (int64_t)row_blocks * 256) {
-    const int i = (int)min(i0 + (threadIdx.x & 63), (int64_t)INT32_MAX), b = find_seq_wave(cu, a.n_seqs, i, n);
-    if (i >= n) continue;
-    const int old = max(a.len[b], 0), pos = old + (i - cu[b]);
-    if (positions) positions[i] = pos;
-    if (slots) {
-      const int entry = pos >> a.page_shift, had = a.pages(old);
-      int page = -1;
-      if (entry < had) page = a.table[(int64_t)b * a.table_stride + entry];
-      else if (entry < a.pages_per_seq) page = taken_page(a, st, grow_first[b] + entry - had);
-      slots[i] = slot_of(a, page, pos);
+  const int n = min(rows, plan->rows), all = rest ? rows : n;
+  for (int64_t i0 = (int64_t)blockIdx.x * 256 + (threadIdx.x & ~63); i0 < all; i0 += (int64_t)row_blocks * 256) {
+    const int i = (int)min(i0 + (threadIdx.x & 63), (int64_t)INT32_MAX);
+    int page = -1, pos = 0;
+    if (i0 < n) {
+      const int b = find_seq_wave(cu, a.n_seqs, i, n);
+      if (i < n) {
+        const int old = max(a.len[b], 0), had = a.pages(old);
+        pos = old + (i - cu[b]);
+        const int entry = pos >> a.page_shift;
+        if (slots && entry < had) page = a.table[(int64_t)b * a.table_stride + entry];
+        else if (slots && entry < a.pages_per_seq) page = taken_page(a, st, grow_first[b] + entry - had);
+      }
+    }
+    if (i < all) {
+      if (positions) positions[i] = pos;
+      if (slots) slots[i] = slot_of(a, page, pos);
     }
   }
 }
@@ -336,6 +342,7 @@ int et_kv_resize(const et_kv_pool *pool, const int32_t *state_dev, int32_t *stat
   const int page = pool->page_size;
   ET_REQUIRE(page >= 16 && page <= 256 && (page & (page - 1)) == 0, "page_size = %d must be 16, 32, 64, 128 or 256", page);
   ET_REQUIRE(pool->n_pages >= 1 && pool->ring_dev != nullptr, "n_pages = %d must be at least 1, and ring_dev not NULL", pool->n_pages);
+  ET_REQUIRE(pool->keep_rest == 0 || pool->keep_rest == 1, "keep_rest = %d must be 0 or 1", pool->keep_rest);
   ET_REQUIRE(state_dev && state_out_dev && (uintptr_t)state_dev % 16 == 0 && (uintptr_t)state_out_dev % 16 == 0,
              "state_dev or state_out_dev is NULL or not aligned to 16 bytes");
   ET_REQUIRE(n_seqs >= 0 && n_seqs <= 1 << 20, "n_seqs = %d must be in [0, 2^20]", n_seqs);
@@ -361,6 +368,7 @@ int et_kv_resize(const et_kv_pool *pool, const int32_t *state_dev, int32_t *stat
     // (3 us).  us, one / several: 256 sequences, 253 rows 6.9 / 5.6; 4, 1544 4.9 / 4.6; 256, 2634 7.0 / 5.1, in place 7.0 / 8.2; in place 4, 5516 7.3 / 7.8;
     // 16, 8550 10.4 / 7.8; 4096, 4096 11.5 / 12.8.  With turns of 2048 rows 16 sequences, 62 605 rows 4.8 -> 5.7, 1000, 8000 5.7 -> 6.8.
     const int turns = std::max(1, (int)(((int64_t)std::max(rows, n_seqs) + kPoolThreads - 1) / kPoolThreads)), fillers = std::min(255, turns);
+    const int fill = pool->keep_rest ? kFill : kFill | kRest;
     const bool in_place = state_out_dev == state_dev, one = in_place && turns <= 6, apart = in_place && !one;
     auto launch = [&](int blocks, int what) {
       (n_seqs <= kPoolThreads ? pool_resize_kernel<1> : pool_resize_kernel<4>)<<<blocks, kPoolThreads, 0, stream>>>(
@@ -369,7 +377,7 @@ int et_kv_resize(const et_kv_pool *pool, const int32_t *state_dev, int32_t *stat
       return ET_OK;
     };
     int rc;
-    if ((rc = launch(one ? 1 : apart ? fillers : fillers + 1, apart ? kFill : kFill | kGive)) || !apart) return rc;
+    if ((rc = launch(one ? 1 : apart ? fillers : fillers + 1, apart ? fill : fill | kGive)) || !apart) return rc;
     return launch(1, kGive);
   }
   PoolPlan *plan = static_cast<PoolPlan *>(workspace_dev);
@@ -377,7 +385,8 @@ int et_kv_resize(const et_kv_pool *pool, const int32_t *state_dev, int32_t *stat
   ET_LAUNCH_CHECK();
   const int row_blocks = positions_dev || slots_dev ? std::min(2048, (int)(((int64_t)rows + 255) / 256)) : 0;
   const int entry_blocks = (int)std::min<int64_t>(256, ((int64_t)n_seqs * pages_per_seq + 255) / 256);
-  pool_fill_kernel<<<row_blocks + entry_blocks, 256, 0, stream>>>(a, cu_rows_dev, plan, rows, row_blocks, positions_dev, slots_dev);
+  pool_fill_kernel<<<row_blocks + entry_blocks, 256, 0, stream>>>(a, cu_rows_dev, plan, rows, !pool->keep_rest, row_blocks, positions_dev,
+                                                                   slots_dev);
   ET_LAUNCH_CHECK();
   return ET_OK;
 }
