@@ -432,7 +432,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_
 }
 
 int launch_paged_mxfp4(int head_dim, const PagedLaunch &l) {
-  const int span = l.window > 0 ? std::min(l.bound, l.window + 15) : l.bound;
+  const int span = l.window > 0 ? (int)std::min<int64_t>(l.bound, (int64_t)l.window + 15) : l.bound;
   // Eight wavefronts where a part is long and a compute unit has one at most, us with eight / four: 9 x 2048 of 24 heads of 128 13.9 / 16.7, of 64
   // 11.3 / 14.2, 32 x 800 of 8 heads of 128 7.8 / 8.9; but 32 x 200 of 4 5.6 / 5.2, 64 x 1500 of 8 20.6 / 19.4.
   const bool wide = l.share == 0 && span > 512 && l.blocks <= 256;
