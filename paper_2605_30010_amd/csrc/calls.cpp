@@ -133,7 +133,11 @@ PyObject *made(int rc, const T &...tensors) {
 }
 template <typename T>
 T *at_address(PyObject *o) { return static_cast<T *>(PyLong_AsVoidPtr(o)); }
-void *stream_of(PyObject *o) { return PyLong_AsVoidPtr(o); }
+// The stream that an argument is (Python's numbers are asked here, with its lock); false, with Python's error: it is none.
+bool stream_of(PyObject *o, void *&stream) {
+  stream = PyLong_AsVoidPtr(o);
+  return stream || !PyErr_Occurred();
+}
 
 #define CALL(name) PyObject *name(PyObject *, PyObject *const *arg, Py_ssize_t)
 
@@ -148,8 +152,10 @@ CALL(append) {
   const at::Tensor *cu = arg[6] == Py_None ? nullptr : ints(arg[6], device, (int64_t)seqs.s.n_seqs + 1);
   if (!cu && arg[6] != Py_None) Py_RETURN_NONE;
   const int32_t *ranges = cu ? static_cast<const int32_t *>(cu->data_ptr()) : nullptr;
+  void *stream;
+  if (!stream_of(arg[7], stream)) return nullptr;
   return done(unlocked([&] {
-    return lib.append(cache, &seqs.s, ranges, (int32_t)k.n, k.data(), k.stride, v.data(), v.stride, stream_of(arg[7]));
+    return lib.append(cache, &seqs.s, ranges, (int32_t)k.n, k.data(), k.stride, v.data(), v.stride, stream);
   }));
   END_HANDLE_TH_ERRORS
 }
@@ -164,9 +170,11 @@ CALL(append_at) {
   if (!k.t || !v.t || !slots || k.n != v.n || k.n > INT32_MAX || k.heads != cache->n_kv_heads || v.heads != cache->n_kv_heads || slots->dim() != 1 ||
       slots->size(0) != k.n || !slots->is_contiguous())
     Py_RETURN_NONE;
+  void *stream;
+  if (!stream_of(arg[5], stream)) return nullptr;
   return done(unlocked([&] {
     return lib.append_slots(cache, static_cast<const int64_t *>(slots->data_ptr()), (int32_t)k.n, k.data(), k.stride, v.data(), v.stride,
-                            stream_of(arg[5]));
+                            stream);
   }));
   END_HANDLE_TH_ERRORS
 }
@@ -185,9 +193,11 @@ CALL(read) {
   const int64_t shape[2] = {rows, width};
   const auto out = fresh({{shape, at::kBFloat16}, {shape, at::kBFloat16}}, device);
   const at::Tensor &k = out[0], &v = out[1];
+  void *stream;
+  if (!stream_of(arg[6], stream)) return nullptr;
   return made(unlocked([&] {
                 return lib.read(cache, &seqs.s, cu ? static_cast<const int32_t *>(cu->data_ptr()) : nullptr, (int32_t)rows,
-                                static_cast<uint16_t *>(k.data_ptr()), width, static_cast<uint16_t *>(v.data_ptr()), width, stream_of(arg[6]));
+                                static_cast<uint16_t *>(k.data_ptr()), width, static_cast<uint16_t *>(v.data_ptr()), width, stream);
               }),
               k, v);
   END_HANDLE_TH_ERRORS
@@ -207,9 +217,11 @@ CALL(attend) {
   const size_t need = lib.attention_bytes(cache, &seqs.s, (int32_t)q.heads, (int32_t)most, (int32_t)window);
   at::Tensor ws;
   if (need) ws = fresh({(int64_t)need}, at::kByte, device);
+  void *stream;
+  if (!stream_of(arg[8], stream)) return nullptr;
   return made(unlocked([&] {
                 return lib.attention(cache, &seqs.s, q.data(), q.stride, (int32_t)q.heads, (int32_t)most, (int32_t)window, scale,
-                                     need ? ws.data_ptr() : nullptr, need, static_cast<uint16_t *>(out.data_ptr()), stream_of(arg[8]));
+                                     need ? ws.data_ptr() : nullptr, need, static_cast<uint16_t *>(out.data_ptr()), stream);
               }),
               out);
   END_HANDLE_TH_ERRORS
@@ -232,12 +244,14 @@ CALL(resize) {
   const size_t need = lib.resize_bytes(seqs.s.n_seqs);
   at::Tensor ws;
   if (need) ws = fresh({(int64_t)need}, at::kByte, device);
+  void *stream;
+  if (!stream_of(arg[8], stream)) return nullptr;
   return made(unlocked([&] {
                 return lib.resize(pool, static_cast<const int32_t *>(state->data_ptr()), static_cast<int32_t *>(state_out->data_ptr()),
                                   const_cast<int32_t *>(seqs.s.page_table_dev), seqs.s.table_stride, seqs.s.pages_per_seq, seqs.s.kv_len_dev,
                                   static_cast<const int32_t *>(fresh_len->data_ptr()), seqs.s.n_seqs, (int32_t)rows,
                                   static_cast<int32_t *>(cu.data_ptr()), static_cast<int32_t *>(positions.data_ptr()),
-                                  static_cast<int64_t *>(slots.data_ptr()), need ? ws.data_ptr() : nullptr, need, stream_of(arg[8]));
+                                  static_cast<int64_t *>(slots.data_ptr()), need ? ws.data_ptr() : nullptr, need, stream);
               }),
               cu, positions, slots);
   END_HANDLE_TH_ERRORS
@@ -280,9 +294,11 @@ CALL(rotate) {
     }
   const at::Tensor *positions = ints(arg[4], device, n);
   if (!positions) Py_RETURN_NONE;
+  void *stream;
+  if (!stream_of(arg[8], stream)) return nullptr;
   const int rc = unlocked([&] {
     return lib.rotary(rotary, static_cast<const int32_t *>(positions->data_ptr()), (int32_t)n, &rows[0], arg[3] == Py_None ? nullptr : &rows[1],
-                      arg[7] == Py_True, stream_of(arg[8]));
+                      arg[7] == Py_True, stream);
   });
   if (rc) return done(rc);
   for (int i = 0; i < 2; ++i) {
