@@ -103,13 +103,15 @@ std::array<at::Tensor, N> fresh(const Wanted (&wanted)[N], long device) {
   }
   return out;
 }
+// Makes the call without Python's lock, which is taken again whatever happens (a tensor whose address
+// torch withholds throws when it is asked).
 template <typename F>
 int unlocked(F &&call) {
-  int rc;
-  Py_BEGIN_ALLOW_THREADS;
-  rc = call();
-  Py_END_ALLOW_THREADS;
-  return rc;
+  struct Released {
+    PyThreadState *state = PyEval_SaveThread();
+    ~Released() { PyEval_RestoreThread(state); }
+  } released;
+  return call();
 }
 PyObject *done(int rc) { return PyLong_FromLong(rc); }
 template <typename... T>
