@@ -470,9 +470,9 @@ int et_kv_resize(const et_kv_pool *pool, const int32_t *state_dev, int32_t *stat
  *     A = 0.1 ln(factor) + 1.
  *   ET_ROTARY_TURNS: the same mix, r falling from 1 to 0 as the number of turns original_len f_i / (2 pi) goes from `slow` to `fast` (1 and 4,
  *     usually).
- * A = 1 but for ET_ROTARY_YARN.  et_rotary_steps (host only) writes f_i as fractions of a turn, steps[i] = round(2^64 f_i / (2 pi)),
+ * A = 1 but for ET_ROTARY_YARN.  et_rotary_steps (host only) writes f_i as fractions of a turn, steps[i] = 2^64 f_i / (2 pi), within two,
  * [rot_dim / 2], and A; the caller puts the steps on the device.  position * steps[i] mod 2^64 is then the angle of any int32
- * position, negative ones too, without loss.  base in [1, 1e30], factor in [1, 1e9]; scaling NULL: none.  Errors: INVALID_ARG. */
+ * position, negative ones too, within 2^-29 radians.  base in [1, 1e30], factor in [1, 1e9]; scaling NULL: none.  Errors: INVALID_ARG. */
 enum { ET_ROTARY_HALF = 0, ET_ROTARY_INTERLEAVED = 1 };
 enum { ET_ROTARY_PLAIN = 0, ET_ROTARY_LINEAR = 1, ET_ROTARY_NTK = 2, ET_ROTARY_YARN = 3, ET_ROTARY_TURNS = 4 };
 typedef struct {

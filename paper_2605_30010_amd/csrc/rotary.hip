@@ -180,7 +180,9 @@ int et_rotary_steps(const et_rotary_scaling *sc, int32_t rot_dim, double base, u
   ET_REQUIRE(kind >= ET_ROTARY_PLAIN && kind <= ET_ROTARY_TURNS, "unknown scaling %d", kind);
   const double factor = kind == ET_ROTARY_PLAIN ? 1.0 : sc->factor;
   ET_REQUIRE(factor >= 1.0 && factor <= 1e9, "factor = %g must be in [1, 1e9]", factor);
-  const double two_pi = 6.283185307179586476925;
+  // (A step counts 2^-64 of a turn, and a far position multiplies its error by 2^31: with the host's 64-bit significands it is within two units, with
+  // double's 53 up to some hundreds.)
+  const long double two_pi = 6.283185307179586476925286766559L;
   const int n = rot_dim;
   if (kind == ET_ROTARY_YARN || kind == ET_ROTARY_TURNS) {
     ET_REQUIRE(sc->original_len >= 1 && sc->original_len <= 1e15, "original_len = %g must be in [1, 1e15]", sc->original_len);
@@ -188,19 +190,21 @@ int et_rotary_steps(const et_rotary_scaling *sc, int32_t rot_dim, double base, u
     ET_REQUIRE(kind != ET_ROTARY_YARN || base > 1.0, "base = %g must be above 1 here", base);
   }
   double first = 0, last = 0;
-  if (kind == ET_ROTARY_NTK && n > 2) base *= std::pow(factor, n / (n - 2.0));
+  long double stretched = base;
+  if (kind == ET_ROTARY_NTK && n > 2) stretched *= std::pow((long double)factor, n / (n - 2.0L));
   if (kind == ET_ROTARY_YARN) {
-    const auto index = [&](double turns) { return n * std::log(sc->original_len / (two_pi * turns)) / (2.0 * std::log(base)); };
+    const auto index = [&](double turns) { return n * std::log(sc->original_len / ((double)two_pi * turns)) / (2.0 * std::log(base)); };
     first = std::max(std::floor(index(sc->fast)), 0.0);
     last = std::min(std::ceil(index(sc->slow)), n - 1.0);
   }
   for (int i = 0; i < n / 2; ++i) {
-    double f = std::pow(base, -2.0 * i / n);
-    double share = kind == ET_ROTARY_LINEAR || (kind == ET_ROTARY_NTK && n == 2) ? 1.0 : 0.0;    // of the frequency that is stretched
-    if (kind == ET_ROTARY_YARN) share = std::min(std::max((i - first) / std::max(last - first, 0.001), 0.0), 1.0);
-    if (kind == ET_ROTARY_TURNS) share = 1.0 - std::min(std::max((sc->original_len * f / two_pi - sc->slow) / (sc->fast - sc->slow), 0.0), 1.0);
-    f = f / factor * share + f * (1.0 - share);
-    steps[i] = (uint64_t)std::nearbyint(f / two_pi * 18446744073709551616.0);          // (f is at most 1: a sixth of a turn)
+    long double f = std::pow(stretched, -2.0L * i / n);
+    long double share = kind == ET_ROTARY_LINEAR || (kind == ET_ROTARY_NTK && n == 2) ? 1.0L : 0.0L;    // of the frequency that is stretched
+    if (kind == ET_ROTARY_YARN) share = std::min(std::max((i - first) / std::max((long double)last - first, 0.001L), 0.0L), 1.0L);
+    if (kind == ET_ROTARY_TURNS)
+      share = 1.0L - std::min(std::max((sc->original_len * f / two_pi - sc->slow) / ((long double)sc->fast - sc->slow), 0.0L), 1.0L);
+    f = f / factor * share + f * (1.0L - share);
+    steps[i] = (uint64_t)std::nearbyint(f / two_pi * 18446744073709551616.0L);         // (f is at most 1: a sixth of a turn)
   }
   *amplitude = kind == ET_ROTARY_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
   return ET_OK;
