@@ -819,7 +819,8 @@ class PagePool(_OnDevice):
         int32 [rows], slots int64 [rows]) of the new tokens, sequence by sequence; `rows` is how many there are, as the caller knows, or a bound:
         rows behind the last sequence's have position 0 and slot -1, for which KVCache.append_at stores nothing.  With `out`, the same three, they
         stay as `out` has them (slots of an earlier call are places still: fill them with -1 before append_at gets them).  The pool's state is changed
-        in place, or goes to state_out int32 [4]: then the call is taken back by going on with the old state and lengths."""
+        in place, or goes to state_out int32 [4]: then the call is taken back by going on with the old state and lengths.  Small results lie
+        apart in one piece of memory: whoever keeps one keeps it all (clone it to keep, save or resize it alone)."""
         s = self._here(stream)
         if s is None:
             with self._elsewhere(stream):
@@ -916,7 +917,7 @@ class Rotary(_OnDevice):
     def apply(self, q, k, positions, out=None, transpose=False, stream=None):
         """Turns q and k, bf16 [rows, heads * head_dim] or [rows, heads, head_dim] (rows may be strided; k may be None), by positions int32
         [rows]; returns both, contiguous, or in `out` = (q, k), which may be q and k themselves.  transpose: by the transposed matrix (the way
-        back, and a gradient's)."""
+        back, and a gradient's).  Small results lie apart in one piece of memory, as PagePool.resize's."""
         s = self._here(stream)
         if s is None:
             with self._elsewhere(stream):

@@ -78,7 +78,8 @@ int64_t whole(PyObject *o, int64_t most) {
 at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type, long device) {
   return at::empty(shape, at::TensorOptions().dtype(type).device(at::Device(at::kCUDA, (c10::DeviceIndex)device)));
 }
-// Several tensors of a call; small ones (up to 8 MiB) in one piece of memory, which costs 0.6 us less for each but the first.
+// Several tensors of a call; small ones (up to 8 MiB) in one piece of memory, which costs 0.6 us less for each but the first (the binding says so where
+// it is done; what is read back from a cache is kept by callers, and is made one by one).
 struct Wanted {
   at::IntArrayRef sizes;
   at::ScalarType type;
@@ -192,9 +193,7 @@ CALL(read) {
   if (!cu && (arg[4] != Py_None || arg[5] != Py_None)) Py_RETURN_NONE;
   const int64_t rows = cu ? whole(arg[5], INT32_MAX) : seqs.s.n_seqs, width = (int64_t)cache->n_kv_heads * cache->head_dim;
   if (rows < 0) Py_RETURN_NONE;
-  const int64_t shape[2] = {rows, width};
-  const auto out = fresh({{shape, at::kBFloat16}, {shape, at::kBFloat16}}, device);
-  const at::Tensor &k = out[0], &v = out[1];
+  const at::Tensor k = fresh({rows, width}, at::kBFloat16, device), v = fresh({rows, width}, at::kBFloat16, device);
   void *stream;
   if (!stream_of(arg[6], stream)) return nullptr;
   return made(unlocked([&] {
