@@ -3,6 +3,7 @@ import ctypes as C
 import importlib
 import math
 import os
+import warnings
 
 import numpy as np
 import torch
@@ -95,15 +96,20 @@ def library_path():
 
 
 def load_library():
-    """Load libearlytom.so and the native part of this binding; raises (never falls back) when they have not been built."""
+    """Load libearlytom.so; raises (never falls back) when it has not been built.  The native part of this binding is built against one torch:
+    where it is missing or does not load, that is said in a warning, and every call goes through Python, to the same kernels."""
     global _lib, _calls
     if _lib is not None:
         return _lib
     if not os.path.exists(_LIB_PATH):
         raise ImportError("libearlytom.so is not built: run `python -c 'import __graft_entry__ as g; "
                           "g.build()'` (or python paper_2605_30010_amd/build.py) first")
-    calls = importlib.import_module(__package__ + "._calls")
-    calls.bind(_LIB_PATH)
+    try:
+        calls = importlib.import_module(__package__ + "._calls")
+        calls.bind(_LIB_PATH)
+    except ImportError as e:
+        calls = None
+        warnings.warn("the binding's native part does not load, small calls take some us more: build again with this torch (%s)" % e, RuntimeWarning)
     lib = C.CDLL(_LIB_PATH)
     i32, i64, f32, vp, sz = C.c_int32, C.c_int64, C.c_float, C.c_void_p, C.c_size_t
     sig = {
