@@ -2,7 +2,7 @@
 // their host part is most of a small call.  A function here makes the call if everything about it is as it mostly is (plain tensors on the
 // device, of the types and layouts asked for) and returns what it makes, or the entry point's error code; for anything else it
 // returns None, and binding.py, which has all the checks and says what is wrong, goes on.  us a call of the binding, launch 2.7 included, without /
-// with this: rotary positions of queries and keys 8.6 / 4.5, a pool's step 10.0 / 5.1, rows stored 6.8 / 4.0, read 8.3 / 4.7, attention 7.2 / 5.0.
+// with this: rotary positions of queries and keys 8.6 / 5.0, a pool's step 10.2 / 5.6, rows stored 7.3 / 4.3, read 8.8 / 5.8, attention 7.7 / 5.1.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <dlfcn.h>

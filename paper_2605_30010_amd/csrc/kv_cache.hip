@@ -191,8 +191,9 @@ __device__ __forceinline__ uint32_t mx_encode8(u32x4 x, uint32_t exponent) {
 // the way to a place is a chain of four loads, so rows share it when there are many.  What is read or written once in long
 // streams (new rows, unquantised cells, rows read back) goes past the caches: 391 MB of e4m3 codes read back 265 -> 254 us, 130 000
 // rows of 4 heads of 80 73 -> 65, 134 MB of bfloat16 rows stored 110 -> 101; codes and the cells of a read do not gain by it.
-// SLOTS: the rows' places are given, in the place of `cu`.  In 4 bits 65 500 rows of 16 heads of 96 are stored in 105 us and read back in 73: 403 MB of
-// rows and 107 of codes and exponents each way, which is what passes the memory side (403 + 111 MB, 5.8 TB/s for both).
+// SLOTS: the rows' places are given, in the place of `cu`.  In 4 bits 65 500 rows of 16 heads of 96, 403 MB of rows and 107 of codes and exponents each way, are
+// stored in 118 us and read back in 131 (81 right behind the store: the cells are in the memory side's cache then; on the same rows again and again 109 and
+// 78).  That is what passes the memory side (403 + 111 MB).
 constexpr int kBatch = 4;
 template <int HD, int FMT, bool STORE, bool SLOTS>
 __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const int32_t *len, const int32_t *table, int n_seqs, int rows,
@@ -222,9 +223,10 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(const int32_t *cu, const i
   const bool in_row = sub * 8 < HD;
   __syncthreads();
   if constexpr (FMT == ET_KV_MXFP4) {
-    // Where a row is whole lines of 128 bytes twice over, a lane has two times eight values, LANES * 8 apart, for one way to them: 4999 rows of 4 heads of
-    // 128 stored and read back 11.0 -> 9.8 us, 90 000 of one of 256 89 -> 84, 131 000 of 8 of 128 117 -> 119 (elsewhere stores of parts of
-    // lines: 65 500 of 16 of 96 181 -> 223).
+    // Where a row is whole lines of 128 bytes twice over, a lane has two times eight values, LANES * 8 apart, for one way to them.  us stored and read
+    // back with one / two, the same rows again and again, and others in turn: 4999 rows of 4 heads of 128 11.0 / 9.6, 11.5 / 11.1; 90 000 of one of 256
+    // level; 16 000 of 4 of 128 18.8 / 20.0, 22.8 / 24.1; 131 000 of 8 of 128 232 / 233, 266 / 287 (elsewhere stores of parts of lines: 65 500 of 16
+    // of 96 181 / 223).
     auto turns = [&](auto batch) {
       constexpr int N = decltype(batch)::value;
       u32x4 x[N][UNITS];

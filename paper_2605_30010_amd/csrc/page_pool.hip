@@ -144,7 +144,7 @@ __device__ __forceinline__ int64_t slot_of(const PoolArgs &a, int page, int pos)
 // rows and look their sequence up there.  kFill: tables, positions, places and row ranges (kRest: of all `rows`, also those behind the last sequence's);
 // kGive: pages given back and the new state, by one workgroup.  The first workgroup gives and the others fill; where the new state takes the old
 // one's place, which the others read, one workgroup does both, or a launch of its own gives.  The loads of a turn are issued together.
-// A step of 256 sequences, some of which end, is two workgroups' chains, 5.5 to 6.1 us (in one 6.9): lengths, sums (two barriers), a search in LDS,
+// A step of 256 sequences, some of which end, is two workgroups' chains, 5.9 to 6.4 us (in one 6.9): lengths, sums (two barriers), a search in LDS,
 // table or ring, result.  A million
 // rows are written in 11 us, 12 bytes each: four such turns of 255 workgroups, one a compute unit (127 / 383 / 511 / 1023 workgroups 14.9 / 13.3 / 12.9 /
 // 17.2 us).  Two or four rows a lane and turn 12.2 / 14.2; 64 registers, so that a compute unit holds two workgroups, 13.0.

@@ -171,7 +171,8 @@ __device__ __forceinline__ void finish_part(const PagedMore &o, const Part &part
 // are exactly; a weight is the sum of two of them, within 2^-15.  A tile's registers are loaded again as soon as they have become operands, so the next
 // tile's keys come in during the softmax and the second product, its values during that and the next logits.  Bound by memory where there is much
 // to read: 64 x 1000 to 16384 tokens of 8 heads of 128, 606 MB in 110 us, 5.5 TB/s, with vector instructions issued 40 % of the time (160 for 32 tokens);
-// 9 x 1 to 2047 of 24 heads of 80, 32 MB in 13.1 us: a start of 4.5 us, then eight turns of what a compute unit gets from memory.  A
+// 9 x 1 to 2047 of 24 heads of 80, 32 MB in 13.1 us: a start of 4.5 us, then the longest part's eight turns, a chain of 0.9 us each (12.4 us where the
+// other eight sequences have one token).  A
 // tile more in flight: 120 -> 118 us there, 13.3 -> 14.0 here, 32 x 0 to 5309 of 4 heads 15.6 -> 16.7; sixteen wavefronts 13.3 -> 14.4.
 template <int HD, bool ONE, int WAVES, int COLS>
 __global__ __launch_bounds__(64 * WAVES, 2) void paged_mxfp4_kernel(const int32_t *len, const int32_t *table, int n_seqs, int share, int bound,
